@@ -414,6 +414,141 @@ int moe_combine(const void* recv, int64_t recv_rows, int32_t hidden, const int32
                 void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The operators around the stage: the norm before it, the router, the order of
+ * the rows by expert, and the experts' products in 8 bits.  All are stateless
+ * and behave as moe_combine does: every argument but the configuration struct is
+ * device memory that the caller owns, tensors are row-major without gaps, the
+ * call enqueues kernels on `stream` (NULL = null stream) and returns without
+ * waiting, an error (MOE_EINVAL, MOE_EUNSUPPORTED, MOE_ECAPACITY, MOE_EHIP)
+ * enqueues nothing and its message is moe_stage_last_error(NULL).  Nothing is
+ * allocated; where an operator needs workspace, a function says how much and the
+ * caller may reuse it for calls that follow on the same stream.  Calls may be
+ * captured in a graph.  Unless said otherwise, outputs are written in full and
+ * may not overlap an input.  16-bit tensors are bf16; they and the int8 ones are
+ * 16-byte aligned, the others (the router's logits among them) to their element.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Root-mean-square norm with the residual's addition, per row of `hidden`:
+ *   h = bf16(x + residual)           (h = x without a residual)
+ *   r = 1 / sqrt(mean(h^2) + eps),   y = h * r * weight       (fp32)
+ *   sum_out = h    out = bf16(y)    rstd = r
+ *   scale = max|y| / 127,  out_q = rne(y * 127 / max|y|)      (int8, never -128)
+ *   x, residual, sum_out, out [rows, hidden] bf16; out_q [rows, hidden] int8;
+ *   weight [hidden] bf16; scale, rstd [rows] fp32.
+ * residual, sum_out, out, (out_q and scale), rstd are optional (NULL), at least one of the
+ * outputs is not.  sum_out and out may each be x or residual itself.  A row of out_q whose
+ * max|y| is below 2^-100 is zeros with scale 0; one with an infinity or a NaN is zeros with
+ * scale NaN (NaN when it is restored).  hidden: a multiple of 8, at most 65536.
+ */
+int moe_norm(const void* x, const void* residual, const void* weight, int64_t rows, int32_t hidden, float eps,
+             void* sum_out, void* out, void* out_q, float* scale, float* rstd, void* stream);
+
+/*
+ * Gradients of moe_norm's out and sum_out, from its sum_out `h` and its rstd:
+ *   g = dy * weight,  dx = bf16(r * (g - h * r^2 * mean(g * h)) + dsum)
+ *   dweight = sum over rows of dy * h * r    (fp32, in a fixed order of rows)
+ * dx [rows, hidden] bf16 is the gradient of x and of residual alike; dsum (optional) is the gradient
+ * that reaches sum_out from elsewhere and may be dx itself.  `workspace` holds at least
+ * moe_norm_backward_workspace(rows, hidden) bytes (16-byte aligned).
+ */
+int64_t moe_norm_backward_workspace(int64_t rows, int32_t hidden);
+int moe_norm_backward(const void* dy, const void* h, const void* weight, const float* rstd, const void* dsum,
+                      int64_t rows, int32_t hidden, void* dx, float* dweight, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/*
+ * bf16 rows to 8 bits with a scale each, as moe_norm makes out_q and scale of its y, and back:
+ * out = bf16(q * scale).  Rows cross between ranks in half the bytes this way, and moe_q8_product
+ * takes them as they are.  hidden: a multiple of 8, at most 65536.
+ */
+int moe_q8_rows(const void* x, int64_t rows, int32_t hidden, void* q, float* scale, void* stream);
+int moe_q8_restore(const void* q, const float* scale, int64_t rows, int32_t hidden, void* out, void* stream);
+
+/* Router configuration.  `experts` fall into `groups` equal runs of consecutive experts. */
+#define MOE_SCORE_SOFTMAX 0
+#define MOE_SCORE_SIGMOID 1
+#define MOE_TYPE_F32 0
+#define MOE_TYPE_BF16 1
+typedef struct {
+  int32_t experts;      /* 1 .. 1024                                                          */
+  int32_t k;            /* choices per token, 1 .. min(experts, 64)                           */
+  int32_t groups;       /* 1 .. 64, divides experts                                           */
+  int32_t top_groups;   /* groups a token may choose from, 1 .. groups                        */
+  int32_t group_best;   /* a group counts by the sum of its best 1 or 2 experts               */
+  int32_t score;        /* MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID                             */
+  int32_t renormalise;  /* 1: a token's weights are its chosen scores over their sum          */
+  float scale;          /* multiplies every weight                                            */
+} moe_route_config_t;
+
+/*
+ * Routing of each token from its logits [tokens, experts] (`logits_type` MOE_TYPE_F32 or _BF16):
+ *   p = softmax(logits) or sigmoid(logits)                       (fp32; the softmax's sum in fp64)
+ *   pick = p + bias                                              (bias [experts] fp32, optional)
+ *   the top_groups groups with the largest sums of their group_best largest picks stay
+ *   ids = the k experts of those with the largest picks, largest first
+ *   weights = scale * p[ids] (/ sum of p[ids], with renormalise)
+ * ids [tokens, k] int32, weights [tokens, k] fp32, scores (optional) p [tokens, experts] fp32.
+ * Equal picks go to the lower index, for experts and for groups.  An expert whose logit or pick is
+ * -infinity is never chosen (its p is 0); where fewer than k are left, the rest of a token's ids are -1
+ * and their weights 0.  Where the chosen scores sum to 0 the weights are 0.  A token with a NaN among
+ * its picks (a NaN logit or bias, or +infinity under a softmax) gets the ids 0 .. k-1 with NaN weights,
+ * so that the error shows in what is computed from it.
+ */
+int moe_route(const moe_route_config_t* cfg, const void* logits, int32_t logits_type, const float* bias, int64_t tokens,
+              int32_t* ids, float* weights, float* scores, void* stream);
+
+/*
+ * Gradient of moe_route's weights (and of its scores, with dscores) by the logits.  The choice itself
+ * has none: `ids` are the forward call's (entries outside [0, experts) have no gradient; ids that repeat
+ * within a token add up).
+ *   dweights [tokens, k] fp32; dscores [tokens, experts] fp32, optional;
+ *   dlogits [tokens, experts] of the logits' type.
+ */
+int moe_route_backward(const moe_route_config_t* cfg, const void* logits, int32_t logits_type, const int32_t* ids,
+                       const float* dweights, const float* dscores, int64_t tokens, void* dlogits, void* stream);
+
+/*
+ * The order of the routed rows by expert: entry (t, j) of ids [tokens, k] is a row of expert ids[t, j];
+ * rows are sorted by (expert, token, choice).
+ *   expert_offsets [experts + 1]  the rows of expert e are [expert_offsets[e], expert_offsets[e + 1])
+ *   row_token [tokens * k]        the token of each row; -1 past the last row
+ *   slot [tokens, k]              the row of each entry, as moe_combine takes it; -1 for an entry outside
+ *                                 [0, experts), which has no row
+ * experts: 1 .. 1024; tokens * k below 2^31.  `workspace` holds at least
+ * moe_group_workspace(tokens * k, experts) bytes (0 for small calls, then NULL will do).
+ */
+int64_t moe_group_workspace(int64_t entries, int32_t experts);
+int moe_group(const int32_t* ids, int64_t tokens, int32_t k, int32_t experts, int32_t* expert_offsets,
+              int32_t* row_token, int32_t* slot, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The experts' products of 8-bit rows and 8-bit weights, summed in 32-bit integers:
+ *   out[i, n] = bf16( float(sum_k xq[r, k] * w[e, n, k]) * (x_scale[r] * w_scale[e, n]) )
+ * for row i of expert e, r = row_index[i] (r = i without row_index):
+ *   xq [x_rows, in_features] int8, x_scale [x_rows] fp32; w [experts, out_features, in_features] int8,
+ *   w_scale [experts, out_features] fp32; out [rows, out_features] bf16.
+ * expert_offsets (device, as moe_group writes it) gives each expert its rows; rows at or past
+ * expert_offsets[experts] are not written.  Without it (NULL) experts has to be 1 and every row is
+ * its.  row_index holds `rows` entries (moe_group's row_token); an entry outside [0, x_rows) makes its
+ * row of out NaN.  Without row_index x_rows has to be at least rows.
+ * in_features: a multiple of 16, at most 131056 (no 32-bit sum overflows); out_features: a multiple
+ * of 8; experts: at most 1024; with row_index x_rows * in_features below 2^32.
+ */
+int moe_q8_product(const void* xq, const float* x_scale, int64_t x_rows, const int32_t* row_index,
+                   const int32_t* expert_offsets, int32_t experts, const void* w, const float* w_scale, int64_t rows,
+                   int32_t in_features, int32_t out_features, void* out, void* stream);
+
+/*
+ * Two such products of the same rows and the gated activation of them:
+ *   out = bf16( silu(g) * u ),  g from w1 and w1_scale, u from w3 and w3_scale  (fp32)
+ */
+int moe_q8_gated(const void* xq, const float* x_scale, int64_t x_rows, const int32_t* row_index,
+                 const int32_t* expert_offsets, int32_t experts, const void* w1, const float* w1_scale, const void* w3,
+                 const float* w3_scale, int64_t rows, int32_t in_features, int32_t out_features, void* out,
+                 void* stream);
+
+/* ---------------------------------------------------------------------------
  * Host-only plan inspection (no GPU needed).  Builds exactly the plan that
  * moe_stage_run would use for these arguments and lets the caller read its
  * tables, so the layout, schedule and combine plan can be checked on a CPU.

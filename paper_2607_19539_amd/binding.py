@@ -33,8 +33,12 @@ ERROR_NAMES = {0: "MOE_OK", -1: "MOE_EINVAL", -2: "MOE_EROUTING", -3: "MOE_ECAPA
 EXPORTED = ["moe_stage_create", "moe_stage_run", "moe_stage_run_serial", "moe_stage_query", "moe_stage_times",
             "moe_stage_last_error", "moe_stage_destroy", "moe_plan_build", "moe_plan_info", "moe_plan_copy",
             "moe_plan_free", "moe_combine", "moe_stage_run_devplan", "moe_stage_run_serial_devplan",
-            "moe_stage_plan_info", "moe_stage_plan_copy", "moe_stage_records", "moe_stage_run_serial_static"]
+            "moe_stage_plan_info", "moe_stage_plan_copy", "moe_stage_records", "moe_stage_run_serial_static",
+            "moe_norm", "moe_norm_backward", "moe_norm_backward_workspace", "moe_q8_rows", "moe_q8_restore", "moe_route",
+            "moe_route_backward", "moe_group", "moe_group_workspace", "moe_q8_product", "moe_q8_gated"]
 MOE_STATIC_SCRATCH_BYTES = 64 * 1024 * 1024
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
+MOE_TYPE_F32, MOE_TYPE_BF16 = 0, 1
 
 
 class moe_stage_config_t(ctypes.Structure):
@@ -42,6 +46,12 @@ class moe_stage_config_t(ctypes.Structure):
                 ("num_ranks", ctypes.c_int32), ("self_rank", ctypes.c_int32), ("max_rows", ctypes.c_int32),
                 ("band_rows", ctypes.c_int32), ("mid_segment_pieces", ctypes.c_int32), ("flags", ctypes.c_uint32),
                 ("watchdog_ms", ctypes.c_int32), ("down_split_k", ctypes.c_int32)]
+
+
+class moe_route_config_t(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("k", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_best", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class moe_stage_stats_t(ctypes.Structure):
@@ -152,6 +162,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.moe_stage_run_serial_static.restype = ctypes.c_int
     lib.moe_stage_records.argtypes = [vp, i32, vp, i64]
     lib.moe_stage_records.restype = ctypes.c_int64
+    f32, rcfg = ctypes.c_float, ctypes.POINTER(moe_route_config_t)
+    lib.moe_norm.argtypes = [vp, vp, vp, i64, i32, f32, vp, vp, vp, vp, vp, vp]
+    lib.moe_norm_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, vp, vp, vp, i64, vp]
+    lib.moe_q8_rows.argtypes = [vp, i64, i32, vp, vp, vp]
+    lib.moe_q8_restore.argtypes = [vp, vp, i64, i32, vp, vp]
+    lib.moe_route.argtypes = [rcfg, vp, i32, vp, i64, vp, vp, vp, vp]
+    lib.moe_route_backward.argtypes = [rcfg, vp, i32, vp, vp, vp, i64, vp, vp]
+    lib.moe_group.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, i64, vp]
+    lib.moe_q8_product.argtypes = [vp, vp, i64, vp, vp, i32, vp, vp, i64, i32, i32, vp, vp]
+    lib.moe_q8_gated.argtypes = [vp, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, i32, i32, vp, vp]
+    lib.moe_norm_backward_workspace.argtypes, lib.moe_group_workspace.argtypes = [i64, i32], [i64, i32]
+    lib.moe_norm_backward_workspace.restype = lib.moe_group_workspace.restype = i64
+    for name in ("moe_norm", "moe_norm_backward", "moe_q8_rows", "moe_q8_restore", "moe_route", "moe_route_backward",
+                 "moe_group", "moe_q8_product", "moe_q8_gated"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("moe_combine", "moe_stage_create", "moe_stage_run", "moe_stage_run_serial", "moe_stage_query",
                  "moe_stage_times", "moe_stage_destroy", "moe_plan_build", "moe_plan_info"):
         getattr(lib, name).restype = ctypes.c_int
@@ -404,6 +429,153 @@ def moe_combine(recv, slot, gate, out, bad_slots=None, stream=None) -> int:
     rc = load().moe_combine(_dev_ptr(recv), rows, H, _dev_ptr(slot), _dev_ptr(gate), T, k, _dev_ptr(out), bad,
                             _stream_ptr(stream))
     return _check(rc)
+
+
+# ----------------------------------------------------------------------------- operators around the stage
+
+def _want(name, t, shape, *dtypes):
+    """Device pointer of a contiguous device tensor of exactly this shape and one of these types (the
+    names of torch's; "bf16" also takes the int16 bit patterns)."""
+    if t.shape != shape or str(t.dtype)[6:] not in dtypes:
+        raise ValueError(f"{name} must be {list(shape)} of {' or '.join(dtypes)}, got {list(t.shape)} of {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    return t.data_ptr()
+
+
+def _opt(name, t, shape, *dtypes):
+    return None if t is None else _want(name, t, shape, *dtypes)
+
+
+_BF16 = ("bfloat16", "int16")
+
+
+def _rows_of(name, t):
+    if len(t.shape) != 2:
+        raise ValueError(f"{name} must have two dimensions, got {list(t.shape)}")
+    return t.shape
+
+
+def _workspace(given, need, stream):
+    """The caller's workspace, or one from torch's allocator: it is the caller's stream that uses it."""
+    if given is not None:
+        if not given.is_cuda or not given.is_contiguous():
+            raise ValueError("workspace must be a contiguous device tensor")
+        return given, given.numel() * given.element_size()
+    if need <= 0:
+        return None, 0
+    import torch
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    if stream is not None:
+        ws.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    return ws, need
+
+
+def moe_norm(x, weight, eps, residual=None, sum_out=None, out=None, out_q=None, scale=None, rstd=None,
+             stream=None) -> int:
+    """Root-mean-square norm of x (+ residual) [T, H] bf16 by weight [H] bf16: the sum in sum_out, the normed
+    rows in out (bf16) or out_q and scale (int8, fp32 [T]), 1 / sqrt(mean square + eps) in rstd (fp32 [T])."""
+    T, H = sh = _rows_of("x", x)
+    args = (_want("x", x, sh, *_BF16), _opt("residual", residual, sh, *_BF16), _want("weight", weight, (H,), *_BF16), T,
+            H, eps, _opt("sum_out", sum_out, sh, *_BF16), _opt("out", out, sh, *_BF16),
+            _opt("out_q", out_q, sh, "int8"), _opt("scale", scale, (T,), "float32"), _opt("rstd", rstd, (T,), "float32"))
+    return _check(load().moe_norm(*args, _stream_ptr(stream)))
+
+
+def moe_norm_backward(dy, h, weight, rstd, dx, dweight, dsum=None, workspace=None, stream=None) -> int:
+    """Gradients of moe_norm: dx [T, H] bf16 and dweight [H] fp32 from dy [T, H], the forward call's sum_out
+    ``h`` and rstd, and the gradient ``dsum`` that reaches sum_out from elsewhere."""
+    T, H = sh = _rows_of("dy", dy)
+    args = (_want("dy", dy, sh, *_BF16), _want("h", h, sh, *_BF16), _want("weight", weight, (H,), *_BF16),
+            _want("rstd", rstd, (T,), "float32"), _opt("dsum", dsum, sh, *_BF16), T, H, _want("dx", dx, sh, *_BF16),
+            _want("dweight", dweight, (H,), "float32"))
+    lib = load()
+    ws, n = _workspace(workspace, lib.moe_norm_backward_workspace(T, H), stream)
+    return _check(lib.moe_norm_backward(*args, ws if ws is None else ws.data_ptr(), n, _stream_ptr(stream)))
+
+
+def moe_q8_rows(x, q, scale, stream=None) -> int:
+    """bf16 rows [T, H] to int8 with one fp32 scale each."""
+    T, H = sh = _rows_of("x", x)
+    return _check(load().moe_q8_rows(_want("x", x, sh, *_BF16), T, H, _want("q", q, sh, "int8"),
+                                     _want("scale", scale, (T,), "float32"), _stream_ptr(stream)))
+
+
+def moe_q8_restore(q, scale, out, stream=None) -> int:
+    """int8 rows [T, H] and their scales back to bf16."""
+    T, H = sh = _rows_of("q", q)
+    return _check(load().moe_q8_restore(_want("q", q, sh, "int8"), _want("scale", scale, (T,), "float32"), T, H,
+                                        _want("out", out, sh, *_BF16), _stream_ptr(stream)))
+
+
+def make_route_config(experts, k, score=MOE_SCORE_SOFTMAX, groups=1, top_groups=1, group_best=1, renormalise=True,
+                      scale=1.0) -> moe_route_config_t:
+    return moe_route_config_t(experts, k, groups, top_groups, group_best, score, int(bool(renormalise)), scale)
+
+
+def _logits(cfg, logits):
+    import torch
+    T, E = _rows_of("logits", logits)
+    if E != cfg.experts:
+        raise ValueError(f"logits must have experts = {cfg.experts} columns, got {E}")
+    kind = MOE_TYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_TYPE_F32
+    return T, E, _want("logits", logits, (T, E), "float32", "bfloat16"), kind
+
+
+def moe_route(cfg: moe_route_config_t, logits, ids, weights, bias=None, scores=None, stream=None) -> int:
+    """Chooses cfg.k experts for each token from logits [T, E] (fp32 or bf16): ids [T, k] int32, weights [T, k]
+    fp32, and, where wanted, the scores [T, E] fp32.  ``bias`` [E] fp32 is added for the choice alone."""
+    T, E, ptr, kind = _logits(cfg, logits)
+    args = (_opt("bias", bias, (E,), "float32"), T, _want("ids", ids, (T, cfg.k), "int32"),
+            _want("weights", weights, (T, cfg.k), "float32"), _opt("scores", scores, (T, E), "float32"))
+    return _check(load().moe_route(ctypes.byref(cfg), ptr, kind, *args, _stream_ptr(stream)))
+
+
+def moe_route_backward(cfg: moe_route_config_t, logits, ids, dweights, dlogits, dscores=None, stream=None) -> int:
+    """Gradient of moe_route's weights (and scores) by the logits, in the logits' type."""
+    T, E, ptr, kind = _logits(cfg, logits)
+    args = (_want("ids", ids, (T, cfg.k), "int32"), _want("dweights", dweights, (T, cfg.k), "float32"),
+            _opt("dscores", dscores, (T, E), "float32"), T, _want("dlogits", dlogits, (T, E), str(logits.dtype)[6:]))
+    return _check(load().moe_route_backward(ctypes.byref(cfg), ptr, kind, *args, _stream_ptr(stream)))
+
+
+def moe_group(ids, experts, expert_offsets, row_token, slot, workspace=None, stream=None) -> int:
+    """Sorts the choices ids [T, k] int32 by expert: expert_offsets [E + 1], the token of each row in row_token
+    [T * k] and the row of each choice in slot [T, k], all int32."""
+    T, k = sh = _rows_of("ids", ids)
+    args = (_want("ids", ids, sh, "int32"), T, k, experts, _want("expert_offsets", expert_offsets, (experts + 1,), "int32"),
+            _want("row_token", row_token, (T * k,), "int32"), _want("slot", slot, sh, "int32"))
+    lib = load()
+    ws, n = _workspace(workspace, lib.moe_group_workspace(T * k, experts), stream)
+    return _check(lib.moe_group(*args, ws if ws is None else ws.data_ptr(), n, _stream_ptr(stream)))
+
+
+def _q8_operands(xq, x_scale, w, w_scale, out, row_index, expert_offsets, name="w"):
+    n, K = _rows_of("xq", xq)
+    rows, N = _rows_of("out", out)
+    E = w.shape[0]
+    if row_index is None and n < rows:
+        raise ValueError(f"xq must have at least out's {rows} rows, got {n}")
+    if expert_offsets is None and E != 1:
+        raise ValueError("expert_offsets is needed with more than one expert")
+    lead = (_want("xq", xq, (n, K), "int8"), _want("x_scale", x_scale, (n,), "float32"), n,
+            _opt("row_index", row_index, (rows,), "int32"), _opt("expert_offsets", expert_offsets, (E + 1,), "int32"), E)
+    mats = (_want(name, w, (E, N, K), "int8"), _want(name + "_scale", w_scale, (E, N), "float32"))
+    return lead, mats, (rows, K, N, _want("out", out, (rows, N), *_BF16))
+
+
+def moe_q8_product(xq, x_scale, w, w_scale, out, row_index=None, expert_offsets=None, stream=None) -> int:
+    """out [rows, N] bf16: 8-bit rows xq [n, K] (taken through row_index, where given) times each expert's weights
+    w [E, N, K], with the scales x_scale [n] and w_scale [E, N]; expert_offsets [E + 1] divides the rows."""
+    lead, mats, tail = _q8_operands(xq, x_scale, w, w_scale, out, row_index, expert_offsets)
+    return _check(load().moe_q8_product(*lead, *mats, *tail, _stream_ptr(stream)))
+
+
+def moe_q8_gated(xq, x_scale, w1, w1_scale, w3, w3_scale, out, row_index=None, expert_offsets=None, stream=None) -> int:
+    """out [rows, N] bf16 = silu(g) * u of the two products g (w1) and u (w3) of the same rows."""
+    lead, mats, tail = _q8_operands(xq, x_scale, w1, w1_scale, out, row_index, expert_offsets, "w1")
+    more = (_want("w3", w3, w1.shape, "int8"), _want("w3_scale", w3_scale, w1_scale.shape, "float32"))
+    return _check(load().moe_q8_gated(*lead, *mats, *more, *tail, _stream_ptr(stream)))
 
 
 def moe_stage_query(h, check: bool = True) -> dict:

@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "../../include/moe_stage.h"
+#include "errors.hpp"
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "plan_device.hpp"
@@ -722,6 +723,15 @@ WsBytes size_workspaces(moe_stage_s* h) {
 }
 
 }  // namespace
+
+int moe::record_error(int code, const char* what, const char* msg) noexcept {
+  try {
+    g_create_error = std::string(what) + ": " + msg;
+  } catch (...) {
+    g_create_error.clear();
+  }
+  return code;
+}
 
 extern "C" {
 
