@@ -6,10 +6,10 @@
 //   gradient: dp_j = scale / P (dw_j - sum_i dw_i p_i / P) (+ dscores),
 //             softmax dl_e = p_e (dp_e - sum dp p),  sigmoid dl_e = dp_e p_e (1 - p_e)
 //
-// One wave takes a token; lane i holds experts i, i + 64, ...  A score has to come out the same however it
-// is computed, or near ties fall differently from one pass (or one launch shape) to the next: expf and the
-// division are the correctly specified ones, and the softmax's sum is taken in 64 bits, whose rounding to 32
-// does not depend on the order of the terms.
+// kLanes lanes take a token; lane i holds the experts i * run .. i * run + run - 1 (run <= kPer) in registers.
+// A score has to come out the same however it is computed, or near ties fall differently from one pass (or one
+// launch shape) to the next: expf and the division are the correctly specified ones, and the softmax's sum is
+// taken in 64 bits, whose rounding to 32 does not depend on the order of the terms.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -22,26 +22,83 @@
 namespace moe {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr float kInf = __builtin_inff();
+constexpr uint32_t kNan = 0x7FC00000u;
 
-__device__ __forceinline__ float load_logit(const RouteArgs& a, int64_t i) {
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float fmax2(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// How a token's experts lie in its lanes.
+template <int kLanes>
+struct Place {
+  int64_t t;      // token
+  bool have;      // t is one of the call's tokens
+  int lane;       // within the token's lanes
+  int run, e0;    // experts per lane, this lane's first
+  int n;          // this lane's experts
+  __device__ __forceinline__ explicit Place(const RouteArgs& a) {
+    constexpr int kTokens = kThreads / kLanes;
+    t = (int64_t)blockIdx.x * kTokens + (int)threadIdx.x / kLanes;
+    have = t < a.tokens;
+    lane = threadIdx.x % kLanes;
+    run = (a.experts + kLanes - 1) / kLanes;
+    e0 = lane * run;
+    n = have ? min(max(a.experts - e0, 0), run) : 0;
+  }
+  // The bits of the token's own lanes in a ballot.
+  __device__ __forceinline__ uint64_t mine(uint64_t ballot) const {
+    if constexpr (kLanes == 64) return ballot;
+    return (ballot >> ((threadIdx.x & 63) / kLanes * kLanes)) & ((1ull << kLanes) - 1);
+  }
+};
+
+__device__ __forceinline__ float logit(const RouteArgs& a, int64_t i) {
   return a.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)a.logits)[i] << 16) : ((const float*)a.logits)[i];
 }
 
-// Scores of the token's experts lane, lane + 64, ... into p; returns with l still the logits.
-template <int kPer>
-__device__ __forceinline__ void scores(const RouteArgs& a, int64_t t, int lane, float (&l)[kPer], float (&p)[kPer]) {
+// The lane's logits; -infinity where it has no expert.  kVec: rows and runs are whole vectors of 16 bytes
+// (fp32) or 8 (bf16).
+template <int kLanes, int kPer, bool kVec>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, const Place<kLanes>& at, float (&l)[kPer]) {
+  const int64_t base = at.t * a.experts + at.e0;
+  if constexpr (kVec) {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 64 * i;
-    l[i] = e < a.experts ? load_logit(a, t * a.experts + e) : -kInf;
-  }
-  if (a.sigmoid) {
+    for (int i = 0; i < kPer; i += 4) {
+      f32x4 v = {-kInf, -kInf, -kInf, -kInf};
+      if (i < at.n) {
+        if (a.bf16) {
+          const u32x2 u = *(const u32x2*)((const uint16_t*)a.logits + base + i);
+          v = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16),
+                    __uint_as_float(u[1] & 0xFFFF0000u)};
+        } else {
+          v = *(const f32x4*)((const float*)a.logits + base + i);
+        }
+      }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) p[i] = 1.0f / (1.0f + expf(-l[i]));
-    return;
+      for (int q = 0; q < 4; ++q) l[i + q] = v[q];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) l[i] = i < at.n ? logit(a, base + i) : -kInf;
   }
+}
+
+// The token's maximum and sum, all that a softmax score needs beside its logit.
+struct Softmax {
+  float m, sum;
+};
+
+__device__ __forceinline__ float score(const RouteArgs& a, float l, const Softmax& s) {
+  if (a.sigmoid) return 1.0f / (1.0f + expf(-l));
+  return s.sum > 0.0f || s.sum != s.sum ? expf(l - s.m) / s.sum : 0.0f;
+}
+
+template <int kLanes, int kPer>
+__device__ __forceinline__ Softmax softmax_of(const RouteArgs& a, const Place<kLanes>& at, const float (&l)[kPer]) {
+  Softmax s{0.0f, 1.0f};
+  if (a.sigmoid) return s;
   float m = -kInf;
   bool nan = false;
 #pragma unroll
@@ -49,197 +106,261 @@ __device__ __forceinline__ void scores(const RouteArgs& a, int64_t t, int lane, 
     m = fmaxf(m, l[i]);
     nan |= l[i] != l[i];
   }
-  m = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
-  if (__any(nan)) m = __uint_as_float(0x7FC00000u);
-  if (m == -kInf) m = 0.0f;  // no expert left: every score is 0
-  double s = 0.0;
+  m = wave_reduce<kLanes>(m, fmax2);
+  s.m = at.mine(__ballot(nan)) ? __uint_as_float(kNan) : m == -kInf ? 0.0f : m;  // no expert left: every score is 0
+  double sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    p[i] = expf(l[i] - m);
-    s += (double)p[i];
-  }
-  s = wave_reduce(s, [](double x, double y) { return x + y; });
-  const float sum = (float)s;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) p[i] = sum > 0.0f || sum != sum ? p[i] / sum : 0.0f;
+  for (int i = 0; i < kPer; ++i) sum += (double)expf(l[i] - s.m);
+  s.sum = (float)wave_reduce<kLanes>(sum, [](double x, double y) { return x + y; });
+  return s;
 }
 
-// A float as an unsigned integer of the same order (-0 counts as 0).
+// A float as an unsigned integer of the same order, above 0 (-0 counts as 0); 0 for -infinity.
 __device__ __forceinline__ uint32_t ordered(float f) {
   const uint32_t u = __float_as_uint(f + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return f == -kInf ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-template <int kPer>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
-  __shared__ float picks[kWaves][1024];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t t = (int64_t)blockIdx.x * kWaves + wave; t < a.tokens; t += (int64_t)gridDim.x * kWaves) {
-    float l[kPer], p[kPer], pick[kPer];
-    scores<kPer>(a, t, lane, l, p);
-    bool nan = false;
+// Leaves the picks of the token's best groups and makes the others -infinity.  A group of a whole power of
+// two of lanes is reduced in registers, another through the wave's LDS.
+template <int kLanes, int kPer>
+__device__ __forceinline__ void keep_groups(const RouteArgs& a, const Place<kLanes>& at, float (&pick)[kPer], float* picks) {
+  const int size = a.experts / a.groups;
+  const int span = size / at.run;  // lanes of a group
+  auto two = [&](float& b0, float& b1, float v) {
+    b1 = fmaxf(b1, fminf(b0, v));
+    b0 = fmaxf(b0, v);
+  };
+  // A group with fewer experts left than count for it is worth nothing (and infinity less infinity is no NaN).
+  auto worth = [&](float b0, float b1) { return a.group_best == 2 ? (b1 == -kInf ? -kInf : b0 + b1) : b0; };
+  if (size % at.run == 0 && (span & (span - 1)) == 0 && span <= 16) {
+    float b0 = -kInf, b1 = -kInf;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 64 * i;
-      pick[i] = -kInf;
-      if (e >= a.experts) continue;
-      if (a.scores) a.scores[t * a.experts + e] = p[i];
-      pick[i] = a.bias ? p[i] + a.bias[e] : p[i];
+    for (int i = 0; i < kPer; ++i) two(b0, b1, pick[i]);
+    auto merge = [&](float o0, float o1) {
+      b1 = fmaxf(fminf(b0, o0), fmaxf(b1, o1));
+      b0 = fmaxf(b0, o0);
+    };
+    if (span >= 2) merge(dpp_of<0xB1>(b0), dpp_of<0xB1>(b1));
+    if (span >= 4) merge(dpp_of<0x4E>(b0), dpp_of<0x4E>(b1));
+    if (span >= 8) merge(dpp_of<0x141>(b0), dpp_of<0x141>(b1));
+    if (span >= 16) merge(dpp_of<0x140>(b0), dpp_of<0x140>(b1));
+    const float value = worth(b0, b1);
+    const int group = at.lane / span;
+    int better = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      const float v = __shfl(value, g * span, kLanes);
+      better += v > value || (v == value && g < group);
+    }
+    if (better >= a.top_groups) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) pick[i] = -kInf;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (i < at.n) picks[at.e0 + i] = pick[i];
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  // Lane g has group g; 16 lanes have up to four each.
+  constexpr int kMost = 64 / kLanes;
+  uint64_t keep = 0;
+  float value[kMost];
+#pragma unroll
+  for (int u = 0; u < kMost; ++u) {
+    const int g = u * kLanes + at.lane;
+    float b0 = -kInf, b1 = -kInf;
+    if (g < a.groups && at.have)
+      for (int i = 0; i < size; ++i) two(b0, b1, picks[g * size + i]);
+    value[u] = worth(b0, b1);
+  }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int u = 0; u < kMost; ++u) {
+    const int mine = u * kLanes + at.lane;
+    int better = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      float v = __shfl(value[0], g, kLanes);
+#pragma unroll
+      for (int o = 1; o < kMost; ++o) {
+        const float w = __shfl(value[o], g, kLanes);
+        if (g / kLanes == o) v = w;
+      }
+      better += v > value[u] || (v == value[u] && g < mine);
+    }
+    keep |= at.mine(__ballot(mine < a.groups && better < a.top_groups)) << (u * kLanes % 64);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (!((keep >> ((at.e0 + i) / size & 63)) & 1)) pick[i] = -kInf;
+}
+
+template <int kLanes, int kPer, bool kVec>
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+  __shared__ float picks[kThreads / kLanes][kLanes * kPer];
+  const Place<kLanes> at(a);
+  float l[kPer], pick[kPer];
+  load_logits<kLanes, kPer, kVec>(a, at, l);
+  const Softmax sm = softmax_of<kLanes, kPer>(a, at, l);
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const float p = score(a, l[i], sm);
+    pick[i] = -kInf;
+    if (i < at.n) {
+      if (a.scores) a.scores[at.t * a.experts + at.e0 + i] = p;
+      pick[i] = a.bias ? p + a.bias[at.e0 + i] : p;
       nan |= pick[i] != pick[i];
       if (l[i] == -kInf) pick[i] = -kInf;
     }
-    if (__any(nan)) {
-      if (lane < a.k) {
-        a.ids[t * a.k + lane] = lane;
-        a.weights[t * a.k + lane] = __uint_as_float(0x7FC00000u);
-      }
-      continue;
-    }
-    if (a.groups > 1) {
-      const int size = a.experts / a.groups;
+  }
+  const bool poisoned = at.mine(__ballot(nan)) != 0;
+  if (a.groups > 1) keep_groups<kLanes, kPer>(a, at, pick, picks[threadIdx.x / kLanes]);
+  // One choice after another: the largest pick, the lowest expert among equals.
+  uint32_t left[kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (lane + 64 * i < a.experts) picks[wave][lane + 64 * i] = pick[i];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      float value = -kInf;
-      if (lane < a.groups) {
-        float b0 = -kInf, b1 = -kInf;
-        for (int i = 0; i < size; ++i) {
-          const float v = picks[wave][lane * size + i];
-          b1 = fmaxf(b1, fminf(b0, v));
-          b0 = fmaxf(b0, v);
-        }
-        value = a.group_best == 2 ? b0 + b1 : b0;
-      }
-      __builtin_amdgcn_wave_barrier();
-      int better = 0;
-      for (int g = 0; g < a.groups; ++g) {
-        const float v = __shfl(value, g);
-        better += v > value || (v == value && g < lane);
-      }
-      const uint64_t keep = __ballot(lane < a.groups && better < a.top_groups);
+  for (int i = 0; i < kPer; ++i) left[i] = ordered(pick[i]);
+  int id = -1;
+  for (int j = 0; j < a.k; ++j) {
+    uint32_t best = left[0];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = lane + 64 * i;
-        if (e < a.experts && !((keep >> (e / size)) & 1)) pick[i] = -kInf;
-      }
-    }
-    // One choice after another: the largest pick, the lowest index among equals.
-    int id = -1;
-    float chosen = 0.0f;
-    for (int j = 0; j < a.k; ++j) {
-      uint64_t best = 0;
+    for (int i = 1; i < kPer; ++i) best = max(best, left[i]);
+    best = wave_reduce<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+    int at_i = kPer;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (pick[i] > -kInf) best = max(best, (uint64_t)ordered(pick[i]) << 32 | (uint32_t)(1023 - (lane + 64 * i)));
-      best = wave_reduce(best, [](uint64_t x, uint64_t y) { return max(x, y); });
-      if (best == 0) break;
-      const int e = 1023 - (int)(uint32_t)best;
-      float v = 0.0f;
+    for (int i = kPer - 1; i >= 0; --i) at_i = left[i] == best ? i : at_i;
+    const int mine = at_i < kPer && best != 0 ? at.e0 + at_i : INT32_MAX;
+    const int e = wave_reduce<kLanes>(mine, [](int x, int y) { return min(x, y); });
+    if (mine != e) at_i = kPer;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (e == lane + 64 * i) {
-          v = p[i];
-          pick[i] = -kInf;
-        }
-      v = __shfl(v, e & 63);
-      if (lane == j) {
-        id = e;
-        chosen = v;
-      }
-    }
-    float w = chosen;
-    if (a.renormalise) {
-      const float total = wave_reduce(chosen, [](float x, float y) { return x + y; });
-      w = total > 0.0f ? chosen / total : 0.0f;
-    }
-    if (lane < a.k) {
-      a.ids[t * a.k + lane] = id;
-      a.weights[t * a.k + lane] = w * a.scale;
-    }
+    for (int i = 0; i < kPer; ++i) left[i] = at_i == i ? 0u : left[i];
+    if (at.lane == j && e != INT32_MAX) id = e;
+  }
+  const bool mine = at.have && at.lane < a.k;
+  if (poisoned) id = at.lane;
+  float chosen = 0.0f;
+  if (mine && id >= 0) chosen = score(a, logit(a, at.t * a.experts + id), sm);
+  float w = chosen;
+  if (a.renormalise) {
+    const float total = wave_reduce<kLanes>(chosen, add);
+    w = total > 0.0f ? chosen / total : 0.0f;
+  }
+  if (mine) {
+    a.ids[at.t * a.k + at.lane] = id;
+    a.weights[at.t * a.k + at.lane] = poisoned ? __uint_as_float(kNan) : w * a.scale;
   }
 }
 
-template <int kPer>
+template <int kLanes, int kPer, bool kVec>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
-  __shared__ float probs[kWaves][1024], grads[kWaves][1024];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t t = (int64_t)blockIdx.x * kWaves + wave; t < a.tokens; t += (int64_t)gridDim.x * kWaves) {
-    float l[kPer], p[kPer];
-    scores<kPer>(a, t, lane, l, p);
+  __shared__ __attribute__((aligned(16))) float table[kThreads / kLanes][kLanes * kPer];
+  const Place<kLanes> at(a);
+  float* grads = table[threadIdx.x / kLanes];
+  float l[kPer], p[kPer], g[kPer];
+  load_logits<kLanes, kPer, kVec>(a, at, l);
+  const int id = at.have && at.lane < a.k ? a.ids[at.t * a.k + at.lane] : -1;
+  const bool have = id >= 0 && id < a.experts;
+  const float dw = have ? a.dweights[at.t * a.k + at.lane] : 0.0f;
+  const Softmax sm = softmax_of<kLanes, kPer>(a, at, l);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 64 * i;
-      if (e >= a.experts) continue;
-      probs[wave][e] = p[i];
-      grads[wave][e] = a.dscores ? a.dscores[t * a.experts + e] : 0.0f;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int id = lane < a.k ? a.ids[t * a.k + lane] : -1;
-    const bool have = id >= 0 && id < a.experts;
-    const float dw = have ? a.dweights[t * a.k + lane] : 0.0f;
-    const float v = have ? probs[wave][id] : 0.0f;
-    float dp = dw * a.scale;
-    if (a.renormalise) {
-      const float total = wave_reduce(v, [](float x, float y) { return x + y; });
-      const float mean = wave_reduce(dw * v, [](float x, float y) { return x + y; }) / total;
-      dp = total > 0.0f || total != total ? a.scale / total * (dw - mean) : 0.0f;
-    }
-    for (int j = 0; j < a.k; ++j)
-      if (lane == j && have) grads[wave][id] += dp;  // one choice at a time: ids may repeat
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    float g[kPer], dot = 0.0f;
+  for (int i = 0; i < kPer; ++i) {
+    p[i] = i < at.n ? score(a, l[i], sm) : 0.0f;
+    grads[at.lane * kPer + i] = i < at.n && a.dscores ? a.dscores[at.t * a.experts + at.e0 + i] : 0.0f;
+  }
+  const float v = have ? score(a, logit(a, at.t * a.experts + id), sm) : 0.0f;
+  float dp = dw * a.scale;
+  if (a.renormalise) {
+    const float total = wave_reduce<kLanes>(v, add);
+    const float mean = wave_reduce<kLanes>(dw * v, add) / total;
+    dp = total > 0.0f || total != total ? a.scale / total * (dw - mean) : 0.0f;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  // One choice at a time, as ids may repeat: a wave's LDS operations happen in their order.
+  const int slot = have ? id / at.run * kPer + id % at.run : 0;
+  for (int j = 0; j < a.k; ++j)
+    if (at.lane == j && have) atomicAdd(&grads[slot], dp);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  float dot = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 64 * i;
-      g[i] = e < a.experts ? grads[wave][e] : 0.0f;
-      dot += e < a.experts ? g[i] * p[i] : 0.0f;
-    }
-    dot = wave_reduce(dot, [](float x, float y) { return x + y; });
+  for (int i = 0; i < kPer; ++i) {
+    g[i] = grads[at.lane * kPer + i];
+    dot += g[i] * p[i];
+  }
+  dot = wave_reduce<kLanes>(dot, add);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = lane + 64 * i;
-      if (e >= a.experts) continue;
-      const float d = a.sigmoid ? g[i] * p[i] * (1.0f - p[i]) : p[i] * (g[i] - dot);
+  for (int i = 0; i < kPer; ++i) g[i] = a.sigmoid ? g[i] * p[i] * (1.0f - p[i]) : p[i] * (g[i] - dot);
+  const int64_t base = at.t * a.experts + at.e0;
+#pragma unroll
+  for (int i = 0; i < kPer; i += kVec ? 4 : 1) {
+    if (i >= at.n) continue;
+    if constexpr (kVec) {
       if (a.bf16)
-        ((uint16_t*)a.dlogits)[t * a.experts + e] = (uint16_t)bf16x2_of(d, 0.0f);
+        *(u32x2*)((uint16_t*)a.dlogits + base + i) = u32x2{bf16x2_of(g[i], g[i + 1]), bf16x2_of(g[i + 2], g[i + 3])};
       else
-        ((float*)a.dlogits)[t * a.experts + e] = d;
+        *(f32x4*)((float*)a.dlogits + base + i) = f32x4{g[i], g[i + 1], g[i + 2], g[i + 3]};
+    } else if (a.bf16) {
+      ((uint16_t*)a.dlogits)[base + i] = (uint16_t)bf16x2_of(g[i], 0.0f);
+    } else {
+      ((float*)a.dlogits)[base + i] = g[i];
     }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
+// Calls f(lanes per token, experts per lane at most, whole vectors) as compile-time values.
 template <class F>
-hipError_t by_experts(const RouteArgs& a, F&& f) {
-  const int per = (a.experts + 63) / 64;
-  const dim3 grid((uint32_t)std::min<int64_t>((a.tokens + kWaves - 1) / kWaves, 1 << 20));
-  if (per <= 1)
-    f(std::integral_constant<int, 1>{}, grid);
-  else if (per <= 2)
-    f(std::integral_constant<int, 2>{}, grid);
-  else if (per <= 4)
-    f(std::integral_constant<int, 4>{}, grid);
-  else if (per <= 8)
-    f(std::integral_constant<int, 8>{}, grid);
+void by_shape(const RouteArgs& a, const void* also, F&& f) {
+  // Sixteen lanes to a token cost the least work in all (a reduction over them is four steps, and four tokens
+  // share each); 64 lanes have the shorter chain, for few tokens.
+  const bool narrow = a.experts <= 256 && a.k <= 16 && a.tokens > 2048;
+  const int run = narrow ? (a.experts + 15) / 16 : (a.experts + 63) / 64;
+  const uintptr_t align = a.bf16 ? 8 : 16;
+  const bool vec = run % 4 == 0 && a.experts % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)also) & (align - 1)) == 0;
+  auto with = [&](auto lanes, auto per) {
+    if constexpr (decltype(per)::value >= 4) {
+      if (vec) return f(lanes, per, std::true_type{});
+    }
+    f(lanes, per, std::false_type{});
+  };
+  auto pick = [&](auto lanes) {
+    if (run <= 1)
+      with(lanes, std::integral_constant<int, 1>{});
+    else if (run <= 2)
+      with(lanes, std::integral_constant<int, 2>{});
+    else if (run <= 4)
+      with(lanes, std::integral_constant<int, 4>{});
+    else if (run <= 8)
+      with(lanes, std::integral_constant<int, 8>{});
+    else
+      with(lanes, std::integral_constant<int, 16>{});
+  };
+  if (narrow)
+    pick(std::integral_constant<int, 16>{});
   else
-    f(std::integral_constant<int, 16>{}, grid);
-  return hipGetLastError();
+    pick(std::integral_constant<int, 64>{});
+}
+
+dim3 token_grid(const RouteArgs& a, int lanes) {
+  const int64_t per = kThreads / lanes;
+  return dim3((uint32_t)((a.tokens + per - 1) / per));
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
-  return by_experts(a, [&](auto per, dim3 grid) {
-    hipLaunchKernelGGL((route_kernel<decltype(per)::value>), grid, dim3(kThreads), 0, s, a);
+  by_shape(a, nullptr, [&](auto lanes, auto per, auto vec) {
+    constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
+    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
   });
+  return hipGetLastError();
 }
 
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s) {
-  return by_experts(a, [&](auto per, dim3 grid) {
-    hipLaunchKernelGGL((route_backward_kernel<decltype(per)::value>), grid, dim3(kThreads), 0, s, a);
+  by_shape(a, a.dlogits, [&](auto lanes, auto per, auto vec) {
+    constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
+    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
   });
+  return hipGetLastError();
 }
 
 }  // namespace moe
