@@ -1,8 +1,10 @@
 // group.hip -- gfx950 kernels of the routed rows' order by expert: a stable counting sort of the choices.
 //
-// Entries are taken in chunks of 64, one wave at a time: entries of one expert within a chunk find each other
-// by ballots over the bits of the expert's number, which gives every entry its rank without an atomic, so the
-// order does not depend on which wave runs first.
+// Workgroup b takes a run of consecutive entries, each of its waves a run of those, 64 at a time.  Entries of one
+// expert among a wave's 64 find each other by ballots over the bits of the expert's number, which ranks them
+// without an atomic, and the wave's count for that expert goes up by their number: the order does not depend on
+// which wave runs first.  Up to kOneEntries one workgroup does it all in one launch; more are counted by a
+// first launch, from whose counts each workgroup of the second finds where its entries of each expert begin.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -13,20 +15,19 @@
 
 namespace moe {
 
-constexpr int kChunk = 64;
-constexpr int kBlockThreads = 256;
-constexpr int kBlockEntries = 1024;
-constexpr int kBlockChunks = kBlockEntries / kChunk;
-constexpr int kOneThreads = 1024;       // the single workgroup: a thread per expert
-constexpr int kOneBytes = 48 * 1024;    // its counts: chunks x experts x 2 bytes
+constexpr int kThreads = 1024;  // a thread for each expert there can be
+constexpr int kWaves = kThreads / 64;
+constexpr int64_t kOneEntries = 4096;
+constexpr int64_t kBlockEntries = 4096;
+constexpr int64_t kMostBlocks = 128;  // each one reads the counts of all of them
 
-inline bool one_workgroup(int64_t n, int32_t experts) {
-  return n <= 8192 && ((n + kChunk - 1) / kChunk) * experts * 2 <= kOneBytes;
+// Entries of a workgroup: a multiple of kThreads.
+inline int64_t block_entries(int64_t n) {
+  const int64_t even = (n + kMostBlocks - 1) / kMostBlocks;
+  return std::max(kBlockEntries, (even + kThreads - 1) / kThreads * kThreads);
 }
 
-int64_t group_blocks(int64_t n, int32_t experts) {
-  return one_workgroup(n, experts) ? 0 : (n + kBlockEntries - 1) / kBlockEntries;
-}
+int64_t group_blocks(int64_t n, int32_t) { return n <= kOneEntries ? 0 : (n + block_entries(n) - 1) / block_entries(n); }
 
 // Lanes of the wave that hold the same id as this one.
 __device__ __forceinline__ uint64_t same_id(uint32_t id, int bits) {
@@ -44,13 +45,13 @@ __device__ __forceinline__ int rank_below(uint64_t m) {
 }
 
 // The expert of entry i; `experts` for an entry that has none.
-__device__ __forceinline__ uint32_t id_of(const GroupArgs& a, int i) {
+__device__ __forceinline__ uint32_t id_of(const GroupArgs& a, int64_t i) {
   if (i >= a.n) return a.experts;
   const uint32_t id = (uint32_t)a.ids[i];
   return id < (uint32_t)a.experts ? id : a.experts;
 }
 
-// Inclusive sum over the workgroup's threads (up to 16 waves).
+// Inclusive sum over the workgroup's threads.
 __device__ __forceinline__ int scan(int v, int* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -64,120 +65,79 @@ __device__ __forceinline__ int scan(int v, int* part) {
   return v;
 }
 
-__global__ __launch_bounds__(kOneThreads) void group_one_kernel(GroupArgs a, int bits) {
-  __shared__ uint16_t cnt[kOneBytes / 2];
-  __shared__ int part[kOneThreads / 64], total;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
-  const int chunks = (a.n + kChunk - 1) / kChunk;
-  for (int i = tid; i < chunks * E; i += kOneThreads) cnt[i] = 0;
+__global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a, int64_t entries) {
+  extern __shared__ int cnt[];  // [experts]
+  const int E = a.experts;
+  for (int e = threadIdx.x; e < E; e += kThreads) cnt[e] = 0;
   __syncthreads();
-  for (int c = wave; c < chunks; c += kOneThreads / 64) {
-    const uint32_t id = id_of(a, c * kChunk + lane);
-    const uint64_t m = same_id(id, bits);
-    if (id < (uint32_t)E && rank_below(m) == 0) cnt[c * E + id] = (uint16_t)__popcll(m);
+  const int64_t first = blockIdx.x * entries;
+  for (int64_t i = first + threadIdx.x; i < first + entries; i += kThreads) {
+    const uint32_t id = id_of(a, i);
+    if (id < (uint32_t)E) atomicAdd(&cnt[id], 1);
   }
   __syncthreads();
-  int sum = 0;
-  if (tid < E)
-    for (int c = 0; c < chunks; ++c) sum += cnt[c * E + tid];
-  const int end = scan(sum, part);
-  if (tid < E) {
-    a.offsets[tid + 1] = end;
-    int at = end - sum;
-    for (int c = 0; c < chunks; ++c) {
-      const int v = cnt[c * E + tid];
-      cnt[c * E + tid] = (uint16_t)at;
-      at += v;
+  for (int e = threadIdx.x; e < E; e += kThreads) a.counts[(int64_t)blockIdx.x * E + e] = (uint32_t)cnt[e];
+}
+
+// kOne: one workgroup, no counts.
+template <bool kOne>
+__global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int64_t entries, int bits) {
+  extern __shared__ int cnt[];  // [kWaves][experts]
+  __shared__ int part[kWaves], total;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
+  const int64_t first = blockIdx.x * entries + wave * (entries / kWaves), end = first + entries / kWaves;
+  int before = 0, all = 0;  // thread e: entries of expert e in earlier workgroups, and in all
+  if (!kOne && tid < E) {
+    const int blocks = gridDim.x, me = blockIdx.x;
+#pragma unroll 8
+    for (int b = 0; b < blocks; ++b) {
+      const int v = (int)a.counts[(int64_t)b * E + tid];
+      all += v;
+      before += b < me ? v : 0;
     }
   }
-  if (tid == 0) a.offsets[0] = 0;
-  if (tid == E - 1) total = end;
+  for (int i = tid; i < kWaves * E; i += kThreads) cnt[i] = 0;
   __syncthreads();
-  for (int c = wave; c < chunks; c += kOneThreads / 64) {
-    const int i = c * kChunk + lane;
+  for (int64_t i = first + lane; i < end; i += 64) {
+    const uint32_t id = id_of(a, i);
+    if (id < (uint32_t)E) atomicAdd(&cnt[wave * E + id], 1);
+  }
+  __syncthreads();
+  if (kOne && tid < E)
+    for (int w = 0; w < kWaves; ++w) all += cnt[w * E + tid];
+  const int upto = scan(all, part);
+  if (tid < E) {
+    int at = upto - all + before;  // the first row of each wave's entries of this expert
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int v = cnt[w * E + tid];
+      cnt[w * E + tid] = at;
+      at += v;
+    }
+    if (blockIdx.x == 0) {
+      a.offsets[tid + 1] = upto;
+      if (tid == 0) a.offsets[0] = 0;
+    }
+  }
+  if (tid == E - 1) total = upto;
+  __syncthreads();
+  for (int64_t i = first + lane; i - lane < end && i - lane < a.n; i += 64) {
     const uint32_t id = id_of(a, i);
     const uint64_t m = same_id(id, bits);
-    if (i >= a.n) continue;
+    const int below = rank_below(m);
+    int pos = -1;
     if (id < (uint32_t)E) {
-      const int pos = cnt[c * E + id] + rank_below(m);
+      pos = cnt[wave * E + id] + below;
+      // Read by all of them, then raised by the first: a wave's LDS operations happen in their order.
+      __builtin_amdgcn_wave_barrier();
+      if (below == 0) cnt[wave * E + id] = pos + (int)__popcll(m);
+      __builtin_amdgcn_wave_barrier();
+      a.row_token[pos] = (int)((uint32_t)i / (uint32_t)a.k);
+    }
+    if (i < a.n) {
       a.slot[i] = pos;
-      a.row_token[pos] = i / a.k;
-    } else {
-      a.slot[i] = -1;
+      if (i >= total) a.row_token[i] = -1;
     }
-  }
-  for (int i = total + tid; i < a.n; i += kOneThreads) a.row_token[i] = -1;
-}
-
-__global__ __launch_bounds__(kBlockThreads) void group_count_kernel(GroupArgs a) {
-  __shared__ uint32_t cnt[1024];
-  const int E = a.experts;
-  for (int e = threadIdx.x; e < E; e += kBlockThreads) cnt[e] = 0;
-  __syncthreads();
-  for (int j = threadIdx.x; j < kBlockEntries; j += kBlockThreads) {
-    const int64_t i = (int64_t)blockIdx.x * kBlockEntries + j;
-    const uint32_t id = i < a.n ? id_of(a, (int)i) : E;
-    if (id < (uint32_t)E) atomicAdd(&cnt[id], 1u);
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kBlockThreads) a.counts[(int64_t)blockIdx.x * E + e] = cnt[e];
-}
-
-// counts[b][e] becomes the first row of block b's entries of expert e.
-__global__ __launch_bounds__(kOneThreads) void group_scan_kernel(GroupArgs a, int blocks) {
-  __shared__ int part[kOneThreads / 64];
-  const int e = threadIdx.x, E = a.experts;
-  int sum = 0;
-  if (e < E)
-    for (int b = 0; b < blocks; ++b) sum += a.counts[(int64_t)b * E + e];
-  const int end = scan(sum, part);
-  if (e == 0) a.offsets[0] = 0;
-  if (e >= E) return;
-  a.offsets[e + 1] = end;
-  int at = end - sum;
-  for (int b = 0; b < blocks; ++b) {
-    const int v = a.counts[(int64_t)b * E + e];
-    a.counts[(int64_t)b * E + e] = at;
-    at += v;
-  }
-}
-
-__global__ __launch_bounds__(kBlockThreads) void group_place_kernel(GroupArgs a, int bits) {
-  __shared__ uint16_t cnt[kBlockChunks * 1024];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
-  const int64_t first = (int64_t)blockIdx.x * kBlockEntries;
-  for (int i = tid; i < kBlockChunks * E; i += kBlockThreads) cnt[i] = 0;
-  __syncthreads();
-  for (int c = wave; c < kBlockChunks; c += kBlockThreads / 64) {
-    const int64_t i = first + c * kChunk + lane;
-    const uint32_t id = i < a.n ? id_of(a, (int)i) : E;
-    const uint64_t m = same_id(id, bits);
-    if (id < (uint32_t)E && rank_below(m) == 0) cnt[c * E + id] = (uint16_t)__popcll(m);
-  }
-  __syncthreads();
-  for (int e = tid; e < E; e += kBlockThreads) {
-    int at = 0;
-    for (int c = 0; c < kBlockChunks; ++c) {
-      const int v = cnt[c * E + e];
-      cnt[c * E + e] = (uint16_t)at;
-      at += v;
-    }
-  }
-  __syncthreads();
-  const int total = a.offsets[E];
-  for (int c = wave; c < kBlockChunks; c += kBlockThreads / 64) {
-    const int64_t i = first + c * kChunk + lane;
-    const uint32_t id = i < a.n ? id_of(a, (int)i) : E;
-    const uint64_t m = same_id(id, bits);
-    if (i >= a.n) continue;
-    if (id < (uint32_t)E) {
-      const int pos = (int)a.counts[(int64_t)blockIdx.x * E + id] + cnt[c * E + id] + rank_below(m);
-      a.slot[i] = pos;
-      a.row_token[pos] = (int)i / a.k;
-    } else {
-      a.slot[i] = -1;
-    }
-    if (i >= total) a.row_token[i] = -1;
   }
 }
 
@@ -185,13 +145,16 @@ hipError_t launch_group(const GroupArgs& a, hipStream_t s) {
   int bits = 1;  // of the numbers 0 .. experts
   while ((a.experts >> bits) != 0) ++bits;
   const int blocks = (int)group_blocks(a.n, a.experts);
+  const uint32_t lds = (uint32_t)(kWaves * a.experts * sizeof(int));
   if (blocks == 0) {
-    hipLaunchKernelGGL(group_one_kernel, dim3(1), dim3(kOneThreads), 0, s, a, bits);
+    const int64_t entries = ((int64_t)a.n + kThreads - 1) / kThreads * kThreads;
+    hipLaunchKernelGGL(group_place_kernel<true>, dim3(1), dim3(kThreads), lds, s, a, entries, bits);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kBlockThreads), 0, s, a);
-  hipLaunchKernelGGL(group_scan_kernel, dim3(1), dim3(kOneThreads), 0, s, a, blocks);
-  hipLaunchKernelGGL(group_place_kernel, dim3(blocks), dim3(kBlockThreads), 0, s, a, bits);
+  const int64_t entries = block_entries(a.n);
+  hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), (uint32_t)(a.experts * sizeof(int)), s, a, entries);
+  if (hipError_t e = hipGetLastError()) return e;
+  hipLaunchKernelGGL(group_place_kernel<false>, dim3(blocks), dim3(kThreads), lds, s, a, entries, bits);
   return hipGetLastError();
 }
 
