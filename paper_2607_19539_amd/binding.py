@@ -333,11 +333,20 @@ def _run_args(x, expert_offsets, row_src_rank, row_slot, w1, w3, w2, return_bufs
     return args, keep
 
 
+@functools.lru_cache(maxsize=None)
+def _current_stream():
+    """A function that returns the current stream's handle, without a Stream object where torch can."""
+    import torch
+    torch.cuda.current_device()  # initialises the device, once
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw and device:
+        return lambda: raw(device())
+    return lambda: torch.cuda.current_stream().cuda_stream
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object
-        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+        return _current_stream()()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -433,21 +442,26 @@ def moe_combine(recv, slot, gate, out, bad_slots=None, stream=None) -> int:
 
 # ----------------------------------------------------------------------------- operators around the stage
 
-def _want(name, t, shape, *dtypes):
-    """Device pointer of a contiguous device tensor of exactly this shape and one of these types (the
-    names of torch's; "bf16" also takes the int16 bit patterns)."""
-    if t.shape != shape or str(t.dtype)[6:] not in dtypes:
-        raise ValueError(f"{name} must be {list(shape)} of {' or '.join(dtypes)}, got {list(t.shape)} of {t.dtype}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous device tensor")
-    return t.data_ptr()
+@functools.lru_cache(maxsize=None)
+def _dtypes():
+    """The tensor types that the operators' arguments may have, by what they hold."""
+    import torch
+    return {"bf16": (torch.bfloat16, torch.int16), "int8": (torch.int8,), "int32": (torch.int32,),
+            "float32": (torch.float32,), "bfloat16": (torch.bfloat16,), "logits": (torch.float32, torch.bfloat16)}
 
 
-def _opt(name, t, shape, *dtypes):
-    return None if t is None else _want(name, t, shape, *dtypes)
+def _want(name, t, shape, kind):
+    """Device pointer of a contiguous device tensor of exactly this shape and kind ("bf16" also takes the
+    int16 bit patterns)."""
+    if t.dtype in _dtypes()[kind] and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype not in _dtypes()[kind] or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} of {kind}, got {list(t.shape)} of {t.dtype}")
+    raise ValueError(f"{name} must be a contiguous device tensor")
 
 
-_BF16 = ("bfloat16", "int16")
+def _opt(name, t, shape, kind):
+    return None if t is None else _want(name, t, shape, kind)
 
 
 def _rows_of(name, t):
@@ -457,7 +471,7 @@ def _rows_of(name, t):
 
 
 def _workspace(given, need, stream):
-    """The caller's workspace, or one from torch's allocator: it is the caller's stream that uses it."""
+    """The caller's workspace, or one from torch's allocator, taken on the stream that will use it."""
     if given is not None:
         if not given.is_cuda or not given.is_contiguous():
             raise ValueError("workspace must be a contiguous device tensor")
@@ -465,10 +479,10 @@ def _workspace(given, need, stream):
     if need <= 0:
         return None, 0
     import torch
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-    if stream is not None:
-        ws.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-    return ws, need
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device="cuda"), need
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return torch.empty(need, dtype=torch.uint8, device="cuda"), need
 
 
 def moe_norm(x, weight, eps, residual=None, sum_out=None, out=None, out_q=None, scale=None, rstd=None,
@@ -476,8 +490,8 @@ def moe_norm(x, weight, eps, residual=None, sum_out=None, out=None, out_q=None, 
     """Root-mean-square norm of x (+ residual) [T, H] bf16 by weight [H] bf16: the sum in sum_out, the normed
     rows in out (bf16) or out_q and scale (int8, fp32 [T]), 1 / sqrt(mean square + eps) in rstd (fp32 [T])."""
     T, H = sh = _rows_of("x", x)
-    args = (_want("x", x, sh, *_BF16), _opt("residual", residual, sh, *_BF16), _want("weight", weight, (H,), *_BF16), T,
-            H, eps, _opt("sum_out", sum_out, sh, *_BF16), _opt("out", out, sh, *_BF16),
+    args = (_want("x", x, sh, "bf16"), _opt("residual", residual, sh, "bf16"), _want("weight", weight, (H,), "bf16"), T,
+            H, eps, _opt("sum_out", sum_out, sh, "bf16"), _opt("out", out, sh, "bf16"),
             _opt("out_q", out_q, sh, "int8"), _opt("scale", scale, (T,), "float32"), _opt("rstd", rstd, (T,), "float32"))
     return _check(load().moe_norm(*args, _stream_ptr(stream)))
 
@@ -486,8 +500,8 @@ def moe_norm_backward(dy, h, weight, rstd, dx, dweight, dsum=None, workspace=Non
     """Gradients of moe_norm: dx [T, H] bf16 and dweight [H] fp32 from dy [T, H], the forward call's sum_out
     ``h`` and rstd, and the gradient ``dsum`` that reaches sum_out from elsewhere."""
     T, H = sh = _rows_of("dy", dy)
-    args = (_want("dy", dy, sh, *_BF16), _want("h", h, sh, *_BF16), _want("weight", weight, (H,), *_BF16),
-            _want("rstd", rstd, (T,), "float32"), _opt("dsum", dsum, sh, *_BF16), T, H, _want("dx", dx, sh, *_BF16),
+    args = (_want("dy", dy, sh, "bf16"), _want("h", h, sh, "bf16"), _want("weight", weight, (H,), "bf16"),
+            _want("rstd", rstd, (T,), "float32"), _opt("dsum", dsum, sh, "bf16"), T, H, _want("dx", dx, sh, "bf16"),
             _want("dweight", dweight, (H,), "float32"))
     lib = load()
     ws, n = _workspace(workspace, lib.moe_norm_backward_workspace(T, H), stream)
@@ -497,7 +511,7 @@ def moe_norm_backward(dy, h, weight, rstd, dx, dweight, dsum=None, workspace=Non
 def moe_q8_rows(x, q, scale, stream=None) -> int:
     """bf16 rows [T, H] to int8 with one fp32 scale each."""
     T, H = sh = _rows_of("x", x)
-    return _check(load().moe_q8_rows(_want("x", x, sh, *_BF16), T, H, _want("q", q, sh, "int8"),
+    return _check(load().moe_q8_rows(_want("x", x, sh, "bf16"), T, H, _want("q", q, sh, "int8"),
                                      _want("scale", scale, (T,), "float32"), _stream_ptr(stream)))
 
 
@@ -505,7 +519,7 @@ def moe_q8_restore(q, scale, out, stream=None) -> int:
     """int8 rows [T, H] and their scales back to bf16."""
     T, H = sh = _rows_of("q", q)
     return _check(load().moe_q8_restore(_want("q", q, sh, "int8"), _want("scale", scale, (T,), "float32"), T, H,
-                                        _want("out", out, sh, *_BF16), _stream_ptr(stream)))
+                                        _want("out", out, sh, "bf16"), _stream_ptr(stream)))
 
 
 def make_route_config(experts, k, score=MOE_SCORE_SOFTMAX, groups=1, top_groups=1, group_best=1, renormalise=True,
@@ -514,12 +528,11 @@ def make_route_config(experts, k, score=MOE_SCORE_SOFTMAX, groups=1, top_groups=
 
 
 def _logits(cfg, logits):
-    import torch
     T, E = _rows_of("logits", logits)
     if E != cfg.experts:
         raise ValueError(f"logits must have experts = {cfg.experts} columns, got {E}")
-    kind = MOE_TYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_TYPE_F32
-    return T, E, _want("logits", logits, (T, E), "float32", "bfloat16"), kind
+    kind = MOE_TYPE_BF16 if logits.dtype in _dtypes()["bfloat16"] else MOE_TYPE_F32
+    return T, E, _want("logits", logits, (T, E), "logits"), kind
 
 
 def moe_route(cfg: moe_route_config_t, logits, ids, weights, bias=None, scores=None, stream=None) -> int:
@@ -535,7 +548,7 @@ def moe_route_backward(cfg: moe_route_config_t, logits, ids, dweights, dlogits, 
     """Gradient of moe_route's weights (and scores) by the logits, in the logits' type."""
     T, E, ptr, kind = _logits(cfg, logits)
     args = (_want("ids", ids, (T, cfg.k), "int32"), _want("dweights", dweights, (T, cfg.k), "float32"),
-            _opt("dscores", dscores, (T, E), "float32"), T, _want("dlogits", dlogits, (T, E), str(logits.dtype)[6:]))
+            _opt("dscores", dscores, (T, E), "float32"), T, _want("dlogits", dlogits, (T, E), "bfloat16" if kind == MOE_TYPE_BF16 else "float32"))
     return _check(load().moe_route_backward(ctypes.byref(cfg), ptr, kind, *args, _stream_ptr(stream)))
 
 
@@ -561,7 +574,7 @@ def _q8_operands(xq, x_scale, w, w_scale, out, row_index, expert_offsets, name="
     lead = (_want("xq", xq, (n, K), "int8"), _want("x_scale", x_scale, (n,), "float32"), n,
             _opt("row_index", row_index, (rows,), "int32"), _opt("expert_offsets", expert_offsets, (E + 1,), "int32"), E)
     mats = (_want(name, w, (E, N, K), "int8"), _want(name + "_scale", w_scale, (E, N), "float32"))
-    return lead, mats, (rows, K, N, _want("out", out, (rows, N), *_BF16))
+    return lead, mats, (rows, K, N, _want("out", out, (rows, N), "bf16"))
 
 
 def moe_q8_product(xq, x_scale, w, w_scale, out, row_index=None, expert_offsets=None, stream=None) -> int:
