@@ -58,30 +58,45 @@ __device__ __forceinline__ float logit(const RouteArgs& a, int64_t i) {
   return a.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)a.logits)[i] << 16) : ((const float*)a.logits)[i];
 }
 
-// The lane's logits; -infinity where it has no expert.  kVec: rows and runs are whole vectors of 16 bytes
-// (fp32) or 8 (bf16).
+// The lane's floats from p on, `none` past its last.
 template <int kLanes, int kPer, bool kVec>
-__device__ __forceinline__ void load_logits(const RouteArgs& a, const Place<kLanes>& at, float (&l)[kPer]) {
-  const int64_t base = at.t * a.experts + at.e0;
+__device__ __forceinline__ void load_floats(const Place<kLanes>& at, const float* p, float none, float (&l)[kPer]) {
   if constexpr (kVec) {
 #pragma unroll
     for (int i = 0; i < kPer; i += 4) {
-      f32x4 v = {-kInf, -kInf, -kInf, -kInf};
-      if (i < at.n) {
-        if (a.bf16) {
-          const u32x2 u = *(const u32x2*)((const uint16_t*)a.logits + base + i);
-          v = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16),
-                    __uint_as_float(u[1] & 0xFFFF0000u)};
-        } else {
-          v = *(const f32x4*)((const float*)a.logits + base + i);
-        }
-      }
+      f32x4 v = {none, none, none, none};
+      if (i < at.n) v = *(const f32x4*)(p + i);
 #pragma unroll
       for (int q = 0; q < 4; ++q) l[i + q] = v[q];
     }
   } else {
 #pragma unroll
+    for (int i = 0; i < kPer; ++i) l[i] = i < at.n ? p[i] : none;
+  }
+}
+
+// The lane's logits; -infinity where it has no expert.  kVec: rows and runs are whole vectors of 16 bytes
+// (fp32) or 8 (bf16).
+template <int kLanes, int kPer, bool kVec>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, const Place<kLanes>& at, float (&l)[kPer]) {
+  const int64_t base = at.t * a.experts + at.e0;
+  if constexpr (!kVec) {
+#pragma unroll
     for (int i = 0; i < kPer; ++i) l[i] = i < at.n ? logit(a, base + i) : -kInf;
+  } else if (a.bf16) {
+    u32x2 v[kPer / 4];
+#pragma unroll
+    for (int i = 0; i < kPer / 4; ++i) {
+      v[i] = u32x2{0xFF80FF80u, 0xFF80FF80u};
+      if (4 * i < at.n) v[i] = *(const u32x2*)((const uint16_t*)a.logits + base + 4 * i);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t u = v[i / 4][i % 4 / 2];
+      l[i] = __uint_as_float(i % 2 ? u & 0xFFFF0000u : u << 16);
+    }
+  } else {
+    load_floats<kLanes, kPer, kVec>(at, (const float*)a.logits + base, -kInf, l);
   }
 }
 
@@ -90,15 +105,16 @@ struct Softmax {
   float m, sum;
 };
 
-__device__ __forceinline__ float score(const RouteArgs& a, float l, const Softmax& s) {
-  if (a.sigmoid) return 1.0f / (1.0f + expf(-l));
+template <bool kSig>
+__device__ __forceinline__ float score(float l, const Softmax& s) {
+  if constexpr (kSig) return 1.0f / (1.0f + expf(-l));
   return s.sum > 0.0f || s.sum != s.sum ? expf(l - s.m) / s.sum : 0.0f;
 }
 
-template <int kLanes, int kPer>
-__device__ __forceinline__ Softmax softmax_of(const RouteArgs& a, const Place<kLanes>& at, const float (&l)[kPer]) {
+template <bool kSig, int kLanes, int kPer>
+__device__ __forceinline__ Softmax softmax_of(const Place<kLanes>& at, const float (&l)[kPer]) {
   Softmax s{0.0f, 1.0f};
-  if (a.sigmoid) return s;
+  if constexpr (kSig) return s;
   float m = -kInf;
   bool nan = false;
 #pragma unroll
@@ -196,24 +212,30 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, const Place<kLan
     if (!((keep >> ((at.e0 + i) / size & 63)) & 1)) pick[i] = -kInf;
 }
 
-template <int kLanes, int kPer, bool kVec>
+template <int kLanes, int kPer, bool kVec, bool kSig>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   __shared__ float picks[kThreads / kLanes][kLanes * kPer];
   const Place<kLanes> at(a);
   float l[kPer], pick[kPer];
   load_logits<kLanes, kPer, kVec>(a, at, l);
-  const Softmax sm = softmax_of<kLanes, kPer>(a, at, l);
+  if (a.bias) {
+    load_floats<kLanes, kPer, kVec>(at, a.bias + at.e0, 0.0f, pick);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) pick[i] = 0.0f;
+  }
+  const Softmax sm = softmax_of<kSig, kLanes, kPer>(at, l);
+  if (a.scores) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i < at.n) a.scores[at.t * a.experts + at.e0 + i] = score<kSig>(l[i], sm);
+  }
   bool nan = false;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const float p = score(a, l[i], sm);
-    pick[i] = -kInf;
-    if (i < at.n) {
-      if (a.scores) a.scores[at.t * a.experts + at.e0 + i] = p;
-      pick[i] = a.bias ? p + a.bias[at.e0 + i] : p;
-      nan |= pick[i] != pick[i];
-      if (l[i] == -kInf) pick[i] = -kInf;
-    }
+    pick[i] += score<kSig>(l[i], sm);
+    nan |= pick[i] != pick[i];
+    if (l[i] == -kInf) pick[i] = -kInf;
   }
   const bool poisoned = at.mine(__ballot(nan)) != 0;
   if (a.groups > 1) keep_groups<kLanes, kPer>(a, at, pick, picks[threadIdx.x / kLanes]);
@@ -227,20 +249,22 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 #pragma unroll
     for (int i = 1; i < kPer; ++i) best = max(best, left[i]);
     best = wave_reduce<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-    int at_i = kPer;
+    // The first of the lane's experts with it; of several lanes' the first lane's, whose experts come first.
+    int found = kPer;
 #pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) at_i = left[i] == best ? i : at_i;
-    const int mine = at_i < kPer && best != 0 ? at.e0 + at_i : INT32_MAX;
-    const int e = wave_reduce<kLanes>(mine, [](int x, int y) { return min(x, y); });
-    if (mine != e) at_i = kPer;
+    for (int i = kPer - 1; i >= 0; --i) found = left[i] == best ? i : found;
+    const uint64_t who = best != 0 ? at.mine(__ballot(found < kPer)) : 0;
+    const int first = __builtin_ctzll(who | 1ull << 63);
+    const int e = __shfl(at.e0 + found, first, kLanes);
+    if (at.lane == j && who != 0) id = e;
+    if (at.lane != first) found = kPer;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) left[i] = at_i == i ? 0u : left[i];
-    if (at.lane == j && e != INT32_MAX) id = e;
+    for (int i = 0; i < kPer; ++i) left[i] = found == i ? 0u : left[i];
   }
   const bool mine = at.have && at.lane < a.k;
   if (poisoned) id = at.lane;
   float chosen = 0.0f;
-  if (mine && id >= 0) chosen = score(a, logit(a, at.t * a.experts + id), sm);
+  if (mine && id >= 0) chosen = score<kSig>(logit(a, at.t * a.experts + id), sm);
   float w = chosen;
   if (a.renormalise) {
     const float total = wave_reduce<kLanes>(chosen, add);
@@ -252,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   }
 }
 
-template <int kLanes, int kPer, bool kVec>
+template <int kLanes, int kPer, bool kVec, bool kSig>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   __shared__ __attribute__((aligned(16))) float table[kThreads / kLanes][kLanes * kPer];
   const Place<kLanes> at(a);
@@ -262,13 +286,19 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   const int id = at.have && at.lane < a.k ? a.ids[at.t * a.k + at.lane] : -1;
   const bool have = id >= 0 && id < a.experts;
   const float dw = have ? a.dweights[at.t * a.k + at.lane] : 0.0f;
-  const Softmax sm = softmax_of<kLanes, kPer>(a, at, l);
+  const float own = have ? logit(a, at.t * a.experts + id) : -kInf;
+  if (a.dscores) {
+    load_floats<kLanes, kPer, kVec>(at, a.dscores + at.t * a.experts + at.e0, 0.0f, g);
+  } else {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    p[i] = i < at.n ? score(a, l[i], sm) : 0.0f;
-    grads[at.lane * kPer + i] = i < at.n && a.dscores ? a.dscores[at.t * a.experts + at.e0 + i] : 0.0f;
+    for (int i = 0; i < kPer; ++i) g[i] = 0.0f;
   }
-  const float v = have ? score(a, logit(a, at.t * a.experts + id), sm) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) grads[at.lane * kPer + i] = g[i];
+  const Softmax sm = softmax_of<kSig, kLanes, kPer>(at, l);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) p[i] = score<kSig>(l[i], sm);
+  const float v = have ? score<kSig>(own, sm) : 0.0f;
   float dp = dw * a.scale;
   if (a.renormalise) {
     const float total = wave_reduce<kLanes>(v, add);
@@ -289,9 +319,9 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
     g[i] = grads[at.lane * kPer + i];
     dot += g[i] * p[i];
   }
-  dot = wave_reduce<kLanes>(dot, add);
+  if constexpr (!kSig) dot = wave_reduce<kLanes>(dot, add);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) g[i] = a.sigmoid ? g[i] * p[i] * (1.0f - p[i]) : p[i] * (g[i] - dot);
+  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * p[i] * (1.0f - p[i]) : p[i] * (g[i] - dot);
   const int64_t base = at.t * a.experts + at.e0;
 #pragma unroll
   for (int i = 0; i < kPer; i += kVec ? 4 : 1) {
@@ -309,20 +339,28 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   }
 }
 
-// Calls f(lanes per token, experts per lane at most, whole vectors) as compile-time values.
+// Calls f(lanes per token, experts per lane at most, whole vectors, sigmoid) as compile-time values; `f32`:
+// fp32 arrays read or written in vectors beside the logits, `also` one of the logits' type.
 template <class F>
-void by_shape(const RouteArgs& a, const void* also, F&& f) {
+void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
   // Sixteen lanes to a token cost the least work in all (a reduction over them is four steps, and four tokens
   // share each); 64 lanes have the shorter chain, for few tokens.
   const bool narrow = a.experts <= 256 && a.k <= 16 && a.tokens > 2048;
   const int run = narrow ? (a.experts + 15) / 16 : (a.experts + 63) / 64;
   const uintptr_t align = a.bf16 ? 8 : 16;
-  const bool vec = run % 4 == 0 && a.experts % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)also) & (align - 1)) == 0;
+  const bool vec = run % 4 == 0 && a.experts % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)also) & (align - 1)) == 0 &&
+                   ((uintptr_t)f32 & 15) == 0;
+  auto kind = [&](auto lanes, auto per, auto v) {
+    if (a.sigmoid)
+      f(lanes, per, v, std::true_type{});
+    else
+      f(lanes, per, v, std::false_type{});
+  };
   auto with = [&](auto lanes, auto per) {
     if constexpr (decltype(per)::value >= 4) {
-      if (vec) return f(lanes, per, std::true_type{});
+      if (vec) return kind(lanes, per, std::true_type{});
     }
-    f(lanes, per, std::false_type{});
+    kind(lanes, per, std::false_type{});
   };
   auto pick = [&](auto lanes) {
     if (run <= 1)
@@ -348,17 +386,17 @@ dim3 token_grid(const RouteArgs& a, int lanes) {
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
-  by_shape(a, nullptr, [&](auto lanes, auto per, auto vec) {
+  by_shape(a, nullptr, a.bias, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
-    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
   });
   return hipGetLastError();
 }
 
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s) {
-  by_shape(a, a.dlogits, [&](auto lanes, auto per, auto vec) {
+  by_shape(a, a.dlogits, a.dscores, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
-    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
   });
   return hipGetLastError();
 }
