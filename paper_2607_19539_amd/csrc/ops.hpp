@@ -88,6 +88,10 @@ hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s);
 // Workgroups that count entries apart from each other; 0: one workgroup does the whole call.
 int64_t group_blocks(int64_t n, int32_t experts);
 hipError_t launch_group(const GroupArgs& a, hipStream_t s);
+// Which kernel takes a product: 16 or 32 features and 16 rows at a time straight from memory (gated: 16 of each
+// matrix), or tiles of 64, 128 or 256 weight rows and as many rows through LDS.
+enum Q8Kind { kQ8Slim1, kQ8Slim2, kQ8Tiles64, kQ8Tiles128, kQ8Tiles256 };
+Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated);
 hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s);
 
 }  // namespace moe

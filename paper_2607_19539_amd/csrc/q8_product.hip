@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "mma_tile.hpp"
 #include "ops.hpp"
@@ -16,16 +17,24 @@
 namespace moe {
 
 constexpr int kThreads = 256;
-constexpr int kRowsTile = kTileM;  // 256 rows of one expert
-constexpr int kWTile = 256;        // weight rows of a tile: features, or 128 gate and 128 up features
-constexpr int kBand = 4;           // tile rows that take turns on one weight tile
-constexpr int kDeal = 32;          // consecutive items that one XCD's compute units run at a time
+constexpr int kBandRows = 1024;  // rows of the tiles that take turns on one weight tile
+constexpr int kDeal = 32;        // consecutive items that one XCD's compute units run at a time
 
-// Epilogue: the finished tile goes through LDS, rows padded by 16 bytes, the scales behind it.
-__host__ __device__ constexpr int out_cols(bool gated) { return gated ? kWTile / 2 : kWTile; }
-__host__ __device__ constexpr int out_stride(bool gated) { return out_cols(gated) * 2 + 16; }
-constexpr int kScales = kRowsTile * out_stride(false);  // kWTile weight scales, then kRowsTile row scales
-static_assert(kScales + (kWTile + kRowsTile) * 4 <= kLdsBytes, "scales behind the staged tile");
+// A workgroup's tile: kW weight rows (features, or as many gate and up features in turn) by up to kX rows.
+// Quarter q of the weight rows is gate (q even) or up (q odd) of the same features, so that a wave, which
+// multiplies a half of them, holds both of a feature; and a wave fetches a quarter, of one matrix.
+template <bool gated, int kW, int kX>
+struct Shape {
+  static constexpr int kCols = gated ? kW / 2 : kW;  // features
+  // Epilogue: the finished tile goes through LDS, rows padded by 16 bytes, the scales behind it.
+  static constexpr int kStride = kCols * 2 + 16;
+  static constexpr int kScales = kX * kStride;
+  static constexpr int kOutBytes = kScales + (kW + kX) * 4;
+  static __device__ __forceinline__ int feature(int n) {
+    return gated ? n / (kW / 2) * (kW / 4) + n % (kW / 4) : n;
+  }
+  static __device__ __forceinline__ bool up(int n) { return gated && (n / (kW / 4)) & 1; }
+};
 
 // silu(g) * u with the hardware exponential and reciprocal, each within about one fp32 ulp (the bf16
 // rounding that follows is 2^-9); a large negative g gives e^-g = inf, a reciprocal of 0 and a result of 0.
@@ -33,152 +42,253 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   return (g * u) * __builtin_amdgcn_rcpf(1.0f + __expf(-g));
 }
 
-// Rows [lo, hi) of expert e from the caller's offsets, which the host cannot check: cut to the rows there
-// are, and never falling (`prev`: where the experts before it end).
-__device__ __forceinline__ void expert_rows(const Q8Args& a, int e, int64_t& lo, int64_t& hi) {
-  lo = min(max((int64_t)a.offsets[e], (int64_t)0), a.rows);
-  hi = min(max((int64_t)a.offsets[e + 1], (int64_t)0), a.rows);
-}
-
 struct Item {
   int expert, col, rows;  // rows: valid rows of the tile, 0: no item
-  int64_t row0;
+  int row0;
 };
 
-template <class T>
-__device__ __forceinline__ T shfl_up_max(T v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v = max(v, o);
-  }
+// v of the lanes up to each, summed.
+__device__ __forceinline__ uint32_t scan_add(uint32_t v) {
+  auto from = [&](auto ctrl, auto rows) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  using std::integral_constant;
+  v += from(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // 1, 2, 4, 8 lanes down within 16
+  v += from(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  v += from(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  v += from(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  v += from(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // lane 15 of a row to the next
+  v += from(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // lane 31 to the upper half
   return v;
 }
 
-// Workgroup b's item.  An expert's items are bands of kBand tile rows by all columns, the rows of a band
+// The rows [lo, hi) of 64 experts from e0 on, an expert a lane, and where the tiles of kTile rows of each end in
+// the running count.  The host cannot check the caller's offsets: they are cut to the rows there are and never
+// fall (`seen`: where the experts before e0 end).
+struct Before {
+  int seen = 0;             // where the experts before these end
+  uint32_t tiles = 0;       // and how many tiles they have
+};
+template <int kTile>
+struct Experts {
+  int lo, hi;
+  uint32_t end;
+  __device__ __forceinline__ Experts(const Q8Args& a, int e0, const Before& b) {
+    const int seen = b.seen;
+    const int lane = threadIdx.x & 63, e = e0 + lane, rows = (int)a.rows;
+    const bool have = e < a.experts;
+    lo = have ? a.offsets[e] : 0;
+    hi = have ? a.offsets[e + 1] : 0;
+    if (__any(have && (lo < seen || hi < lo || hi > rows))) {
+      int m = have ? min(max(max(lo, hi), seen), rows) : seen;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(m, d);
+        if (lane >= d) m = max(m, o);
+      }
+      const int start = __shfl_up(m, 1);
+      lo = lane == 0 ? min(max(lo, seen), m) : max(start, min(lo, m));
+      hi = m;
+      if (!have) lo = hi;
+    }
+    end = b.tiles + scan_add((uint32_t)(hi - lo + kTile - 1) / kTile);
+  }
+  __device__ __forceinline__ Before after(const Q8Args& a, int e0) const {
+    return Before{__builtin_amdgcn_readlane(hi, min(a.experts - e0, 64) - 1), (uint32_t)__builtin_amdgcn_readlane((int)end, 63)};
+  }
+};
+
+// Workgroup b's item.  An expert's items are bands of kBandRows rows by all columns, the tiles of a band
 // next to each other; items are dealt to the XCDs (workgroups b, b + 8, ... share one) in runs of kDeal, so
 // that the compute units of an XCD read the same few weight and row tiles through its L2.  Every wave finds
 // the item by itself: 64 experts at a time, a lane each.
+template <int kTile>
 __device__ __forceinline__ Item find_item(const Q8Args& a, uint32_t b, int cols) {
-  const int lane = threadIdx.x & 63;
+  constexpr uint32_t kBand = kBandRows / kTile;
   const uint32_t xcd = b % kXcds, j = b / kXcds;
-  if (!a.offsets) {
-    const int64_t tiles = (a.rows + kRowsTile - 1) / kRowsTile;
-    const uint32_t total = (uint32_t)(tiles * cols);
+  // The item's number, of `total`.
+  auto dealt = [&](uint32_t total) {
     const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
-    const uint32_t it = ((j / run) * kXcds + xcd) * run + j % run;
-    if (it >= total) return Item{0, 0, 0, 0};
-    const uint32_t band = it / (uint32_t)(kBand * cols), q = it % (uint32_t)(kBand * cols);
-    const int64_t t0 = (int64_t)band * kBand;
-    const uint32_t nb = (uint32_t)min((int64_t)kBand, tiles - t0);
-    const int64_t row0 = (t0 + q % nb) * kRowsTile;
-    return Item{0, (int)(q / nb), (int)min((int64_t)kRowsTile, a.rows - row0), row0};
-  }
-  // Tile rows of every expert: a running sum, twice (the deal needs the total first).
-  int64_t seen = 0;
-  uint32_t before = 0;
-  auto chunk = [&](int e0, int64_t& lo, int64_t& hi, uint32_t& end) {
-    const int e = e0 + lane;
-    lo = hi = 0;
-    if (e < a.experts) expert_rows(a, e, lo, hi);
-    hi = max(shfl_up_max(max(lo, hi), lane), seen);
-    const int64_t ends = __shfl_up(hi, 1);
-    lo = max(lo, lane == 0 ? seen : max(ends, seen));
-    if (e >= a.experts) lo = hi;
-    const uint32_t n = (uint32_t)((hi - lo + kRowsTile - 1) / kRowsTile);
-    end = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(end, d);
-      if (lane >= d) end += o;
-    }
-    end += before;
+    return ((j / run) * kXcds + xcd) * run + j % run;
   };
-  for (int e0 = 0; e0 < a.experts; e0 += 64) {
-    int64_t lo, hi;
-    uint32_t end;
-    chunk(e0, lo, hi, end);
-    seen = __shfl(hi, 63);
-    before = __shfl(end, 63);
+  auto item = [&](int expert, int lo, int hi, uint32_t tiles, uint32_t q) {
+    const uint32_t band = q / (kBand * cols), in = q % (kBand * cols);
+    const uint32_t nb = min(kBand, tiles - band * kBand);
+    const int row0 = lo + (int)(band * kBand + in % nb) * kTile;
+    return Item{expert, (int)(in / nb), min(kTile, hi - row0), row0};
+  };
+  using X = Experts<kTile>;
+  const Item none{0, 0, 0, 0};
+  if (!a.offsets) {
+    const uint32_t tiles = (uint32_t)((a.rows + kTile - 1) / kTile), it = dealt(tiles * cols);
+    return it < tiles * cols ? item(0, 0, (int)a.rows, tiles, it) : none;
   }
-  const uint32_t total = before * (uint32_t)cols;
-  if (total == 0) return Item{0, 0, 0, 0};
-  const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
-  const uint32_t it = ((j / run) * kXcds + xcd) * run + j % run;
-  if (it >= total) return Item{0, 0, 0, 0};
-  seen = 0;
-  before = 0;
-  for (int e0 = 0; e0 < a.experts; e0 += 64) {
-    int64_t lo, hi;
-    uint32_t end;
-    chunk(e0, lo, hi, end);
-    const uint64_t past = __ballot(it < end * (uint32_t)cols);
-    if (past != 0) {
-      const int l = __builtin_ctzll(past);
-      const uint32_t prev = __shfl_up(end, 1);
-      const uint32_t first = __builtin_amdgcn_readfirstlane(l == 0 ? before : __shfl(prev, l));
-      const uint32_t tiles = __builtin_amdgcn_readfirstlane(__shfl(end, l)) - first;
-      const int64_t elo = __shfl(lo, l), ehi = __shfl(hi, l);
-      const uint32_t local = it - first * (uint32_t)cols;
-      const uint32_t band = local / (uint32_t)(kBand * cols), q = local % (uint32_t)(kBand * cols);
-      const uint32_t nb = min((uint32_t)kBand, tiles - band * kBand);
-      const int64_t row0 = elo + (int64_t)(band * kBand + q % nb) * kRowsTile;
-      return Item{e0 + l, (int)(q / nb), (int)min((int64_t)kRowsTile, ehi - row0), row0};
-    }
-    seen = __shfl(hi, 63);
-    before = __shfl(end, 63);
+  // The tiles of all experts are counted first: the deal goes by their number.
+  auto pick = [&](const X& x, int e0, const Before& b, uint32_t it, Item& found) {
+    const uint64_t past = __ballot(it < x.end * cols);
+    if (past == 0) return false;
+    const int l = __builtin_ctzll(past);
+    const uint32_t first = l == 0 ? b.tiles : (uint32_t)__builtin_amdgcn_readlane((int)x.end, l - 1);
+    const uint32_t tiles = (uint32_t)__builtin_amdgcn_readlane((int)x.end, l) - first;
+    found = item(e0 + l, __builtin_amdgcn_readlane(x.lo, l), __builtin_amdgcn_readlane(x.hi, l), tiles, it - first * cols);
+    return true;
+  };
+  Item found = none;
+  if (a.experts <= 64) {
+    const X x(a, 0, Before{});
+    const uint32_t total = x.after(a, 0).tiles * cols;
+    if (total == 0) return none;
+    const uint32_t it = dealt(total);
+    if (it < total) pick(x, 0, Before{}, it, found);
+    return found;
   }
-  return Item{0, 0, 0, 0};
+  Before all;
+  for (int e0 = 0; e0 < a.experts; e0 += 64) all = X(a, e0, all).after(a, e0);
+  const uint32_t total = all.tiles * cols;
+  if (total == 0) return none;
+  const uint32_t it = dealt(total);
+  if (it >= total) return none;
+  Before past;
+  for (int e0 = 0; e0 < a.experts; e0 += 64) {
+    const X x(a, e0, past);
+    if (pick(x, e0, past, it, found)) return found;
+    past = x.after(a, e0);
+  }
+  return none;
 }
 
 // The item in scalar registers: it is the same in every lane.
 __device__ __forceinline__ Item uniform(const Item& it) {
   return Item{__builtin_amdgcn_readfirstlane(it.expert), __builtin_amdgcn_readfirstlane(it.col),
-              __builtin_amdgcn_readfirstlane(it.rows),
-              (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(it.row0 >> 32)) << 32 |
-                        (uint32_t)__builtin_amdgcn_readfirstlane((int)it.row0))};
+              __builtin_amdgcn_readfirstlane(it.rows), __builtin_amdgcn_readfirstlane(it.row0)};
 }
 
-// One tile of kRows rows (of which it.rows are valid) by kWTile weight rows.
-template <bool gated, int kRows>
+// kW weight rows by kX rows in two by two waves, for products too small for whole tiles: a ring of four K steps.
+// A step's second half of fragments is read under the products of the first; the barrier between the two ends
+// every wave's reads of the step, whose slot is filled again at once, and the next step's first half is read under
+// the products of the second.
+template <int kW, int kX>
+__device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, DmaRows<kW / 32>& w, DmaRows<kX / 32>& x, int K,
+                                          const ChunkTail& tail, i32x4 (&acc)[kW / 32][kX / 32]) {
+  constexpr int kStages = 4, kNI = kW / 32, kNJ = kX / 32;
+  constexpr uint32_t kStageBytes = (kW + kX) * kRowBytes;
+  constexpr int kDmaStage = kNI + kNJ;
+  const int tid = item_thread(), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lk = lane >> 4;
+  const uint32_t lane_chunk = (uint32_t)lr * kRowBytes + (((uint32_t)lk ^ swz(lr)) << 4);
+  const uint32_t a_lane = (uint32_t)((wave & 1) * (kW / 2)) * kRowBytes + lane_chunk;
+  const uint32_t b_lane = (uint32_t)(kW + (wave >> 1) * (kX / 2)) * kRowBytes + lane_chunk;
+#pragma unroll
+  for (int i = 0; i < kNI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) acc[i][j] = i32x4{};
+  const int nk = ChunkTail::steps(K);
+  const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kNI * 1024;
+  const uint32_t lds_x = lds_addr(lds) + kW * kRowBytes + (uint32_t)wave * kNJ * 1024;
+  int loaded = 0;
+  uint32_t st_load = 0, st_use = 0;
+  auto next = [](uint32_t st) { return st == (kStages - 1) * kStageBytes ? 0u : st + kStageBytes; };
+  auto load = [&]() {
+    static_for<kNI>([&](auto q) {
+      dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w + st_load);
+    });
+    static_for<kNJ>([&](auto q) {
+      dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x + st_load);
+    });
+    advance_to(w, x, ++loaded, nk, tail);
+    st_load = next(st_load);
+  };
+  i32x4 fa[2][kNI], fb[2][kNJ];
+  auto read = [&](int kk) {
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) fb[kk][j] = *(const i32x4*)(lds + ((b_lane ^ ((uint32_t)kk << 6)) + st_use + j * 16 * kRowBytes));
+#pragma unroll
+    for (int i = 0; i < kNI; ++i) fa[kk][i] = *(const i32x4*)(lds + ((a_lane ^ ((uint32_t)kk << 6)) + st_use + i * 16 * kRowBytes));
+  };
+  auto multiply = [&](int kk) {
+#pragma unroll
+    for (int i = 0; i < kNI; ++i)
+#pragma unroll
+      for (int j = 0; j < kNJ; ++j) I8Mma::mma(acc[i][j], fa[kk][i], fb[kk][j]);
+  };
+  // ahead: K steps behind the next one that may still be in flight; -1: there is no next step.
+  auto step = [&](auto ahead, auto fetch) {
+    constexpr int n = decltype(ahead)::value;
+    read(1);
+    if constexpr (n < 0) {
+      mask_chunks(tail, 0, lk, fa[0]);
+      mask_chunks(tail, 1, lk, fa[1]);
+    }
+    multiply(0);
+    if constexpr (n >= 0) {
+      wait_vm_and_barrier<n * kDmaStage>();
+      st_use = next(st_use);
+      if constexpr (decltype(fetch)::value) load();
+      read(0);
+    }
+    multiply(1);
+  };
+  using std::false_type;
+  advance_to(w, x, 0, nk, tail);
+  for (int ks = 0; ks < min(nk, kStages); ++ks) load();
+  if (nk >= 4)
+    wait_vm_and_barrier<3 * kDmaStage>();
+  else if (nk == 3)
+    wait_vm_and_barrier<2 * kDmaStage>();
+  else if (nk == 2)
+    wait_vm_and_barrier<kDmaStage>();
+  else
+    wait_vm_and_barrier<0>();
+  read(0);
+  for (int ks = 0; ks + kStages < nk; ++ks) step(std::integral_constant<int, 2>{}, std::true_type{});
+  if (nk >= 4) step(std::integral_constant<int, 2>{}, false_type{});
+  if (nk >= 3) step(std::integral_constant<int, 1>{}, false_type{});
+  if (nk >= 2) step(std::integral_constant<int, 0>{}, false_type{});
+  step(std::integral_constant<int, -1>{}, false_type{});
+  mfma_drain(acc);
+  wait_vm_and_barrier<0>();
+}
+
+// One tile of kW weight rows by kX rows, of which it.rows are valid.
+template <bool gated, int kW, int kX>
 __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t* lds) {
-  constexpr bool kNarrow = kRows <= 64;
-  constexpr int kNI = kNarrow ? 4 : 8;
-  constexpr int kNJ = kNarrow ? kRows / 16 : kRows / 32;
-  constexpr int kDmaX = kRows / 32;
+  using S = Shape<gated, kW, kX>;
+  constexpr bool kNarrow = kW == 256 && kX <= 64;       // four waves by the weight rows alone
+  constexpr int kNI = kNarrow ? 4 : kW / 32;            // weight fragments per wave
+  constexpr int kNJ = kNarrow ? kX / 16 : kX / 32;      // row fragments per wave
+  constexpr int kDmaW = kW / 32, kDmaX = kX / 32;       // DMA instructions per wave and K step
   const int tid = item_thread(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lk = lane >> 4;
   const int K = a.K, N = a.N;
   auto quad_n = [&](int i) {
     return kNarrow ? (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16 + 4 * lk
-                   : (wave & 1) * 128 + i * 16 + 4 * lk;
+                   : (wave & 1) * (kW / 2) + i * 16 + 4 * lk;
   };
-  auto quad_m = [&](int j) { return (kNarrow ? 0 : (wave >> 1) * (kRows / 2)) + j * 16 + lr; };
-  // Tile row n is feature first + n, or, gated, rows 0..63 and 128..191 are gate features and the 64 rows
-  // after each the up rows of the same features: a wave holds both of a feature.
-  const int first = it.col * out_cols(gated);
-  auto feature = [&](int n) { return gated ? first + (n >> 7) * 64 + (n & 63) : first + n; };
+  auto quad_m = [&](int j) { return (kNarrow ? 0 : (wave >> 1) * (kX / 2)) + j * 16 + lr; };
+  const int first = it.col * S::kCols;
+  auto feature = [&](int n) { return min(first + S::feature(n), N - 1); };
   const uint32_t r8 = (uint32_t)lane >> 3;
   const int cmax = min(K / 16, 8) - 1;
-  DmaRows<kDmaPerThread> w;
+  DmaRows<kDmaW> w;
   DmaRows<kDmaX> x;
   w.step = x.step = kRowBytes;
   const int64_t wofs = (int64_t)it.expert * N;
   {
-    const int f0 = min(feature(wave * 64), N - 1);
-    w.base = (const uint8_t*)(gated && (wave & 1) ? a.w3 : a.w) + (wofs + f0) * K;
+    const int f0 = feature(wave * (kW / 4));
+    w.base = (const uint8_t*)(S::up(wave * (kW / 4)) ? a.w3 : a.w) + (wofs + f0) * K;
 #pragma unroll
-    for (int i = 0; i < kDmaPerThread; ++i) {
-      const uint32_t n = (uint32_t)(8 * i) + r8;
+    for (int i = 0; i < kDmaW; ++i) {
+      const uint32_t n = (uint32_t)(wave * (kW / 4) + 8 * i) + r8;
       const uint32_t c = min(((uint32_t)lane & 7) ^ swz(n), (uint32_t)cmax);
-      w.off[i] = (uint32_t)(min(feature(wave * 64 + (int)n), N - 1) - f0) * (uint32_t)K + (c << 4);
+      w.off[i] = (uint32_t)(feature((int)n) - f0) * (uint32_t)K + (c << 4);
     }
   }
   // A row that row_index does not name takes row 0 (any readable one) and a scale of NaN.
   auto source = [&](int m, bool& ok) {
-    const int64_t i = it.row0 + min(m, it.rows - 1);
-    const int64_t r = a.index ? (int64_t)a.index[i] : i;
+    const int i = it.row0 + min(m, it.rows - 1);
+    const int64_t r = a.index ? a.index[i] : i;
     ok = r >= 0 && r < a.x_rows;
     return ok ? r : (int64_t)0;
   };
@@ -192,14 +302,13 @@ __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t
     const int64_t r = source((int)n, ok);
     x.off[i] = (ok ? (uint32_t)(r - xrow0) * (uint32_t)K : 0u) + (c << 4);
   }
-  float my_xs, my_ws;
-  {
+  float my_xs = 0.0f, my_ws = 0.0f;
+  if (tid < kX) {
     bool ok;
     const int64_t r = source(tid, ok);
     my_xs = ok ? a.xs[r] : __uint_as_float(0x7FC00000u);
-    const int f = min(feature(tid), N - 1);
-    my_ws = (gated && ((tid >> 6) & 1) ? a.ws3 : a.ws)[wofs + f];
   }
+  if (tid < kW) my_ws = (S::up(tid) ? a.ws3 : a.ws)[wofs + feature(tid)];
   // Offsets and scales are complete before the first operand DMA, which the compiler does not count.
 #pragma unroll
   for (int i = 0; i < kDmaX; ++i) asm volatile("" ::"v"(x.off[i]));
@@ -210,23 +319,24 @@ __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t
   auto nothing = [] {};
   if constexpr (kNarrow)
     narrow_mma<I8Mma, kNJ>(lds, w, x, K, tail, acc, nothing);
-  else
+  else if constexpr (kW == 256)
     tile_mma<I8Mma, kNJ>(lds, w, x, K, tail, acc, nothing);
+  else
+    small_mma<kW, kX>(lds, w, x, K, tail, acc);
 
-  float* scales = (float*)(lds + kScales);
-  scales[tid] = my_ws;
-  scales[kWTile + tid] = my_xs;
+  float* scales = (float*)(lds + S::kScales);
+  if (tid < kW) scales[tid] = my_ws;
+  if (tid < kX) scales[kW + tid] = my_xs;
   __syncthreads();
-  constexpr int kStride = out_stride(gated);
   float xs[kNJ];
 #pragma unroll
-  for (int j = 0; j < kNJ; ++j) xs[j] = scales[kWTile + quad_m(j)];
+  for (int j = 0; j < kNJ; ++j) xs[j] = scales[kW + quad_m(j)];
 #pragma unroll
   for (int i = 0; i < (gated ? kNI / 2 : kNI); ++i) {
     const int n = quad_n(i);
     const f32x4 ws = *(const f32x4*)(scales + n);
     f32x4 ws3 = {};
-    if constexpr (gated) ws3 = *(const f32x4*)(scales + n + 64);
+    if constexpr (gated) ws3 = *(const f32x4*)(scales + n + kW / 4);
 #pragma unroll
     for (int j = 0; j < kNJ; ++j) {
       float v[4];
@@ -235,53 +345,263 @@ __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t
         v[q] = (float)acc[i][j][q] * (xs[j] * ws[q]);
         if constexpr (gated) v[q] = silu_mul(v[q], (float)acc[i + kNI / 2][j][q] * (xs[j] * ws3[q]));
       }
-      const int fl = gated ? (n >> 7) * 64 + (n & 63) : n;
-      *(u32x2*)(lds + quad_m(j) * kStride + fl * 2) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
+      *(u32x2*)(lds + quad_m(j) * S::kStride + S::feature(n) * 2) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
       __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
     }
   }
   __syncthreads();
-  constexpr int kLanes = out_cols(gated) / 8;  // threads that store one row
+  constexpr int kLanes = S::kCols / 8;  // threads that store one row
   const int c8 = tid % kLanes;
   const int f = first + c8 * 8;
   if (f < N) {
 #pragma unroll 4
-    for (int p = 0; p < kRows * kLanes / kThreads; ++p) {
+    for (int p = 0; p < kX * kLanes / kThreads; ++p) {
       const int m = p * (kThreads / kLanes) + tid / kLanes;
-      if (m < it.rows) *(u32x4*)(a.out + (it.row0 + m) * N + f) = *(const u32x4*)(lds + m * kStride + c8 * 16);
+      if (m < it.rows) *(u32x4*)(a.out + (int64_t)(it.row0 + m) * N + f) = *(const u32x4*)(lds + m * S::kStride + c8 * 16);
     }
   }
 }
 
 template <bool gated>
 __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(Q8Args a, int cols) {
+  static_assert(Shape<gated, 256, 256>::kOutBytes <= kLdsBytes, "staged tile");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
-  const Item it = uniform(find_item(a, blockIdx.x, cols));
+  const Item it = uniform(find_item<256>(a, blockIdx.x, cols));
   const int rows = it.rows;
   if (rows <= 0) return;
   if (rows <= 32)
-    q8_item<gated, 32>(a, it, lds);
+    q8_item<gated, 256, 32>(a, it, lds);
   else if (rows <= 64)
-    q8_item<gated, 64>(a, it, lds);
+    q8_item<gated, 256, 64>(a, it, lds);
   else if (rows <= 128)
-    q8_item<gated, 128>(a, it, lds);
+    q8_item<gated, 256, 128>(a, it, lds);
   else if (rows <= 192)
-    q8_item<gated, 192>(a, it, lds);
+    q8_item<gated, 256, 192>(a, it, lds);
   else
-    q8_item<gated, 256>(a, it, lds);
+    q8_item<gated, 256, 256>(a, it, lds);
+}
+
+template <bool gated, int kW, int kX>
+__global__ __launch_bounds__(kThreads, kW + kX <= 128 ? 2 : 1) void q8_small_kernel(Q8Args a, int cols) {
+  constexpr int kRing = 4 * (kW + kX) * kRowBytes, kOut = Shape<gated, kW, kX>::kOutBytes;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing > kOut ? kRing : kOut];
+  const Item it = uniform(find_item<kX>(a, blockIdx.x, cols));
+  if (it.rows <= 0) return;
+  q8_item<gated, kW, kX>(a, it, lds);
+}
+
+// ------------------------------------------------------------------------------------ few rows
+
+// Row tile t of the experts' rows cut into runs of kTile.
+template <int kTile>
+__device__ __forceinline__ Item find_rows(const Q8Args& a, uint32_t t) {
+  if (!a.offsets) return Item{0, 0, min(kTile, (int)a.rows - (int)t * kTile), (int)t * kTile};
+  Before b;
+  for (int e0 = 0; e0 < a.experts; e0 += 64) {
+    const Experts<kTile> x(a, e0, b);
+    const uint64_t past = __ballot(t < x.end);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
+      const uint32_t first = l == 0 ? b.tiles : (uint32_t)__builtin_amdgcn_readlane((int)x.end, l - 1);
+      const int row0 = __builtin_amdgcn_readlane(x.lo, l) + (int)(t - first) * kTile;
+      return Item{e0 + l, 0, min(kTile, __builtin_amdgcn_readlane(x.hi, l) - row0), row0};
+    }
+    b = x.after(a, e0);
+  }
+  return Item{0, 0, 0, 0};
+}
+
+// A tile of 16 kR rows by 16 kN features (gated: kN of each matrix): the four waves take every fourth 128 bytes
+// of K each, straight from memory into registers, so nothing in the loop waits for another wave, and add their
+// sums up in LDS at the end.
+template <bool gated, int kN, int kR>
+__global__ __launch_bounds__(kThreads) void q8_slim_kernel(Q8Args a) {
+  constexpr int kM = gated ? 2 : 1;
+  constexpr int kFrags = kM * kN * kR;
+  constexpr int kWaves = kThreads / 64;
+  __shared__ i32x4 sums[kWaves][kFrags][64];
+  const Item it = uniform(find_rows<16 * kR>(a, blockIdx.y));
+  if (it.rows <= 0) return;
+  const int lane = threadIdx.x & 63, lr = lane & 15, lk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int K = a.K, N = a.N, n0 = blockIdx.x * 16 * kN;
+  const int64_t wofs = (int64_t)it.expert * N;
+  const int8_t* wp[kM][kN];
+  const int8_t* xp[kR];
+#pragma unroll
+  for (int m = 0; m < kM; ++m)
+#pragma unroll
+    for (int i = 0; i < kN; ++i) wp[m][i] = (m ? a.w3 : a.w) + (wofs + min(n0 + i * 16 + lr, N - 1)) * K + lk * 16;
+#pragma unroll
+  for (int j = 0; j < kR; ++j) {
+    const int i = it.row0 + min(j * 16 + lr, it.rows - 1);
+    const int64_t r = a.index ? a.index[i] : i;
+    const bool ok = r >= 0 && r < a.x_rows;
+    xp[j] = (ok ? a.x + r * K : a.w) + lk * 16;
+  }
+  i32x4 acc[kM][kN][kR];
+#pragma unroll
+  for (int m = 0; m < kM; ++m)
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int j = 0; j < kR; ++j) acc[m][i][j] = i32x4{};
+  struct Chunk {
+    i32x4 w[2][kM][kN], x[2][kR];
+  };
+  auto load = [&](Chunk& c, int k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int m = 0; m < kM; ++m)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) c.w[h][m][i] = *(const i32x4*)(wp[m][i] + k + h * 64);
+#pragma unroll
+      for (int j = 0; j < kR; ++j) c.x[h][j] = *(const i32x4*)(xp[j] + k + h * 64);
+    }
+  };
+  auto multiply = [&](const Chunk& c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int m = 0; m < kM; ++m)
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+#pragma unroll
+          for (int j = 0; j < kR; ++j)
+            acc[m][i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(c.w[h][m][i], c.x[h][j], acc[m][i][j], 0, 0, 0);
+  };
+  const int nfull = K / 128;
+  Chunk c0, c1;
+  int c = wave;
+  if (c < nfull) load(c0, c * 128);
+  while (c < nfull) {
+    if (c + kWaves < nfull) load(c1, (c + kWaves) * 128);
+    multiply(c0);
+    c += kWaves;
+    if (c >= nfull) break;
+    if (c + kWaves < nfull) load(c0, (c + kWaves) * 128);
+    multiply(c1);
+    c += kWaves;
+  }
+  if (K % 128 && wave == nfull % kWaves) {  // the last chunks of 16 bytes
+    const int k = nfull * 128;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = k + h * 64 + lk * 16 < K;
+#pragma unroll
+      for (int m = 0; m < kM; ++m)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          c0.w[h][m][i] = i32x4{};
+          if (in) c0.w[h][m][i] = *(const i32x4*)(wp[m][i] + k + h * 64);
+        }
+#pragma unroll
+      for (int j = 0; j < kR; ++j) {
+        c0.x[h][j] = i32x4{};
+        if (in) c0.x[h][j] = *(const i32x4*)(xp[j] + k + h * 64);
+      }
+    }
+    multiply(c0);
+  }
+#pragma unroll
+  for (int m = 0; m < kM; ++m)
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int j = 0; j < kR; ++j) sums[wave][(i * kR + j) * kM + m][lane] = acc[m][i][j];
+  __syncthreads();
+#pragma unroll
+  for (int f = 0; f < kN * kR; ++f) {
+    if (f % kWaves != wave) continue;
+    const int i = f / kR, j = f % kR;
+    const int n = n0 + i * 16 + 4 * lk, m = j * 16 + lr;
+    if (n >= N || m >= it.rows) continue;
+    const int64_t row = it.row0 + m;
+    const int64_t r = a.index ? (int64_t)a.index[row] : row;
+    const float xs = r >= 0 && r < a.x_rows ? a.xs[r] : __uint_as_float(0x7FC00000u);
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < kM; ++q) {
+      i32x4 s = sums[0][f * kM + q][lane];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) s += sums[w][f * kM + q][lane];
+      const float* ws = (q ? a.ws3 : a.ws) + wofs + n;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float p = (float)s[t] * (xs * ws[t]);
+        v[t] = q ? silu_mul(v[t], p) : p;
+      }
+    }
+    *(u32x2*)(a.out + row * N + n) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
+  }
+}
+
+template <bool gated, int kN>
+hipError_t launch_slim(const Q8Args& a, hipStream_t s) {
+  const int64_t tiles = (a.rows + 15) / 16 + (a.offsets ? std::min<int64_t>(a.experts, a.rows) : 0);
+  if (tiles > 65535) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((q8_slim_kernel<gated, kN, 1>), dim3((a.N + 16 * kN - 1) / (16 * kN), (uint32_t)tiles), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool gated, int kW, int kX>
+hipError_t launch_tiles(const Q8Args& a, hipStream_t s) {
+  // Tiles there can be: every expert may end in a partly filled one.
+  const int64_t tiles = (a.rows + kX - 1) / kX + (a.offsets ? std::min<int64_t>(a.experts, a.rows) : 0);
+  const int cols = (a.N + Shape<gated, kW, kX>::kCols - 1) / Shape<gated, kW, kX>::kCols;
+  const int64_t grid = (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
+  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  if constexpr (kW == 256)
+    hipLaunchKernelGGL(q8_tile_kernel<gated>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
+  else
+    hipLaunchKernelGGL((q8_small_kernel<gated, kW, kX>), dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
+  return hipGetLastError();
+}
+
+Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated) {
+  // What each kernel would take, in microseconds, from the rows an expert has on average (the host does not know
+  // the offsets): the rounds of tiles over 256 compute units, each so many K steps of 128 bytes and something
+  // for its start and end, as measured on single matrices; and the reading of every weight, at the rate that the
+  // kernel reached where that is all.
+  const double nk = (K + kRowBytes - 1) / kRowBytes, features = (double)N * (gated ? 2 : 1);
+  const double busy = grouped ? experts * (1.0 - std::pow(1.0 - 1.0 / experts, (double)rows)) : 1.0;
+  const double per = rows / busy, megabytes = busy * features * K * 1e-6;
+  auto tiles = [&](double x) { return grouped ? busy * (1.0 + std::max(0.0, (per - x / 2) / x)) : std::ceil(rows / x); };
+  auto items = [&](double w, double x) { return tiles(x) * std::ceil(features / w) / 256.0; };
+  auto cost = [&](double work, double rate) { return std::max(work, megabytes / rate) + 0.3 * work; };
+  const double whole = items(256, 256), half = items(128, 128), quarter = items(64, 64);
+  const double height = std::min(256.0, std::max(32.0, per));
+  const double step = (0.2 + 1.185 * height / 256) * std::min(1.0, 0.7 + 0.3 * whole);
+  Q8Kind best = kQ8Tiles256;
+  double least = cost(2 + std::ceil(whole) * (nk * step + 6), 4.8);
+  auto consider = [&](Q8Kind kind, double c) {
+    if (c < least) best = kind, least = c;
+  };
+  consider(kQ8Tiles128, cost(2 + std::ceil(half) * (nk * 0.61 + 1), 4.6));
+  consider(kQ8Tiles64, cost(3 + std::max(1.0, quarter) * (nk * 0.2 + 0.3), 5.2));
+  if (tiles(16) <= 65535) {
+    const double slim = items(gated ? 32 : 16, 16), slim2 = items(32, 16);
+    consider(kQ8Slim1, cost(2 + nk * std::max(0.1, (gated ? 0.14 : 0.12) * slim), 5.8));
+    if (!gated) consider(kQ8Slim2, cost(2 + nk * std::max(0.16, 0.16 * slim2), 5.8));
+  }
+  return best;
 }
 
 hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s) {
-  // Tiles there can be: every expert may end in a partly filled one.
-  const int64_t tiles = (a.rows + kRowsTile - 1) / kRowsTile + (a.offsets ? std::min<int64_t>(a.experts, a.rows) : 0);
-  const int cols = (a.N + out_cols(gated) - 1) / out_cols(gated);
-  const int64_t grid = (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (gated)
-    hipLaunchKernelGGL(q8_tile_kernel<true>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
-  else
-    hipLaunchKernelGGL(q8_tile_kernel<false>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
-  return hipGetLastError();
+  switch (q8_kind(a.rows, a.offsets != nullptr, a.experts, a.K, a.N, gated)) {
+    case kQ8Slim1:
+      return gated ? launch_slim<true, 1>(a, s) : launch_slim<false, 1>(a, s);
+    case kQ8Slim2:
+      return launch_slim<false, 2>(a, s);
+    case kQ8Tiles64:
+      return gated ? launch_tiles<true, 64, 64>(a, s) : launch_tiles<false, 64, 64>(a, s);
+    case kQ8Tiles128:
+      return gated ? launch_tiles<true, 128, 128>(a, s) : launch_tiles<false, 128, 128>(a, s);
+    case kQ8Tiles256:
+      break;
+  }
+  return gated ? launch_tiles<true, 256, 256>(a, s) : launch_tiles<false, 256, 256>(a, s);
 }
 
 }  // namespace moe
