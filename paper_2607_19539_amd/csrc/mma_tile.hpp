@@ -229,9 +229,39 @@ __device__ __forceinline__ void mfma_drain(Acc (&acc)[kNI][kNJ]) {
 // waits for step ks+1's blocks, with only block 2ks+4 allowed in flight.  The last two K steps are
 // peeled so each wait count is a constant on a straight path.
 // ---------------------------------------------------------------------------
-template <class Op, int kNJ, class Tail, class Late>
-__device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
-                                         const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Late&& late) {
+
+// The DMAs of a K step: weights to lds_w, tokens to lds_x (this wave's parts of their blocks).
+template <int kDmaW, int kDmaX>
+__device__ __forceinline__ void fetch_step(const DmaRows<kDmaW>& w, const DmaRows<kDmaX>& x, uint32_t lds_w, uint32_t lds_x) {
+  static_for<kDmaW>([&](auto q) {
+    dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w);
+  });
+  static_for<kDmaX>([&](auto q) { dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x); });
+}
+
+// Prologue: K steps 0 and 1 in flight.  w.base and x.base then point at the next step to fetch.  The ring has to be
+// free; nothing is waited for, so the DMAs may run under what the caller does before tile_run.
+template <int kNJ, class Tail>
+__device__ __forceinline__ void tile_start(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
+                                           const Tail& tail) {
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  const int nk = Tail::steps(K);
+  const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
+  const uint32_t lds_x = lds_addr(lds) + (uint32_t)wave * kNJ * 1024;
+  advance_to(w, x, 0, nk, tail);
+  fetch_step(w, x, lds_w, lds_x + kBlockBytes);
+  advance_to(w, x, 1, nk, tail);
+  if (nk > 1) {
+    fetch_step(w, x, lds_w + 2 * kBlockBytes, lds_x + 3 * kBlockBytes);
+    advance_to(w, x, 2, nk, tail);
+  }
+}
+
+// The K loop after tile_start: late() two K steps (or one) before the end, last() before the last step, when every
+// DMA has arrived.
+template <class Op, int kNJ, class Tail, class Late, class Last>
+__device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
+                                         const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Late&& late, Last&& last) {
   typedef typename Op::Frag Frag;
   static_assert(kNJ == 4 || kNJ == 6 || kNJ == 8, "token fragments per wave");
   constexpr int kHJ = kNJ / 2;
@@ -266,24 +296,11 @@ __device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDma
     fb[j] = *(const Frag*)(lds + ((b_lane ^ ((uint32_t)kk << 6)) + slot + j * 16 * kRowBytes));
   };
 
-  // Prologue: K steps 0 and 1 in flight, step 0 visible, its first sub-step read.  w.base and x.base
-  // then point at the next step to fetch.
-  auto fetch = [&](uint32_t sw, uint32_t sx) {
-    static_for<kDmaPerThread>([&](auto q) {
-      dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w + sw);
-    });
-    static_for<kNJ>([&](auto q) { dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x + sx); });
-  };
-  advance_to(w, x, 0, nk, tail);
-  fetch(o0, o1);
-  advance_to(w, x, 1, nk, tail);
-  if (nk > 1) {
-    fetch(o2, o3);
-    advance_to(w, x, 2, nk, tail);
+  // Step 0 visible, its first sub-step read.
+  if (nk > 1)
     wait_vm_and_barrier<kDmaPerThread + kNJ>();
-  } else {
+  else
     wait_vm_and_barrier<0>();
-  }
 #pragma unroll
   for (int j = 0; j < kHJ; ++j) read_b(o1, 0, j);
 #pragma unroll
@@ -352,10 +369,18 @@ __device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDma
   for (; ks + 2 < nk; ++ks) step(std::integral_constant<int, 0>{});
   late();  // two K steps (or one) before the end
   if (ks + 1 < nk) step(std::integral_constant<int, 1>{});
+  last();
   step(std::integral_constant<int, 2>{});
   mfma_drain(acc);
   // All waves are done reading LDS before the epilogue or the next tile reuses it.
   wait_vm_and_barrier<0>();
+}
+
+template <class Op, int kNJ, class Tail, class Late>
+__device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
+                                         const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Late&& late) {
+  tile_start(lds, w, x, K, tail);
+  tile_run<Op>(lds, w, x, K, tail, acc, late, [] {});
 }
 
 // ---------------------------------------------------------------------------
@@ -368,13 +393,33 @@ __device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDma
 // acc[i][j] holds n = (wave/2)*128 + (i/2)*64 + (wave%2)*32 + (i%2)*16 + 4*(lane/16) + r (a gate
 // row block and its up rows in the same wave), m = j*16 + lane%16.
 // ---------------------------------------------------------------------------
-template <class Op, int kNB, class Tail, class Late>
-__device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNB / 2>& x,
-                                           int K, const Tail& tail, typename Op::Acc (&acc)[4][kNB], Late&& late) {
+constexpr int kNarrowStages = 4;
+template <int kNB>
+constexpr uint32_t kNarrowStageBytes = kBlockBytes + 16 * kNB * kRowBytes;
+
+// Prologue: up to three K steps in flight, nothing waited for.
+template <int kNB, class Tail>
+__device__ __forceinline__ void narrow_start(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNB / 2>& x, int K,
+                                             const Tail& tail) {
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  const int nk = Tail::steps(K);
+  const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
+  const uint32_t lds_x = lds_addr(lds) + kBlockBytes + (uint32_t)wave * (kNB / 2) * 1024;
+  advance_to(w, x, 0, nk, tail);
+  for (int ks = 0; ks < min(nk, kNarrowStages - 1); ++ks) {
+    fetch_step(w, x, lds_w + ks * kNarrowStageBytes<kNB>, lds_x + ks * kNarrowStageBytes<kNB>);
+    advance_to(w, x, ks + 1, nk, tail);
+  }
+}
+
+// The K loop after narrow_start: late() three K steps (or fewer) before the end, last() before the last one's.
+template <class Op, int kNB, class Tail, class Late, class Last>
+__device__ __forceinline__ void narrow_run(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNB / 2>& x, int K,
+                                           const Tail& tail, typename Op::Acc (&acc)[4][kNB], Late&& late, Last&& last) {
   typedef typename Op::Frag Frag;
   static_assert(kNB == 2 || kNB == 4, "token fragments per wave");
-  constexpr int kStages = 4;
-  constexpr uint32_t kStageBytes = kBlockBytes + 16 * kNB * kRowBytes;
+  constexpr int kStages = kNarrowStages;
+  constexpr uint32_t kStageBytes = kNarrowStageBytes<kNB>;
   static_assert(kStages * kStageBytes <= (uint32_t)kLdsBytes, "ring of K steps");
   constexpr int kDmaX = kNB / 2;
   constexpr int kDmaStage = kDmaPerThread + kDmaX;
@@ -394,16 +439,11 @@ __device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kD
   const int nk = Tail::steps(K);
   const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
   const uint32_t lds_x = lds_addr(lds) + kBlockBytes + (uint32_t)wave * kDmaX * 1024;
-  int loaded = 0;                    // K steps fetched
-  uint32_t st_load = 0, st_use = 0;  // ring offsets of the next step to fetch and to multiply
+  int loaded = min(nk, kStages - 1);                              // K steps fetched
+  uint32_t st_load = (uint32_t)loaded * kStageBytes, st_use = 0;  // ring offsets of the next step to fetch and to multiply
   auto next = [](uint32_t st) { return st == (kStages - 1) * kStageBytes ? 0u : st + kStageBytes; };
   auto load = [&]() {
-    static_for<kDmaPerThread>([&](auto q) {
-      dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w + st_load);
-    });
-    static_for<kDmaX>([&](auto q) {
-      dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x + st_load);
-    });
+    fetch_step(w, x, lds_w + st_load, lds_x + st_load);
     advance_to(w, x, ++loaded, nk, tail);
     st_load = next(st_load);
   };
@@ -431,8 +471,6 @@ __device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kD
 #pragma unroll
         for (int j = 0; j < kNB; ++j) Op::mma(acc[i][j], fa[kk][i], fb[kk][j]);
   };
-  advance_to(w, x, 0, nk, tail);
-  for (int ks = 0; ks < min(nk, kStages - 1); ++ks) load();
   int ks = 0;
   for (; ks + kStages - 1 < nk; ++ks) {
     wait_vm_and_barrier<2 * kDmaStage>();  // step ks visible; every wave has read step ks-1
@@ -450,10 +488,18 @@ __device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kD
     multiply(std::false_type{});
   }
   wait_vm_and_barrier<0>();
+  last();
   multiply(std::true_type{});
   mfma_drain(acc);
   // All waves are done reading LDS before the epilogue or the next tile reuses it.
   wait_vm_and_barrier<0>();
+}
+
+template <class Op, int kNB, class Tail, class Late>
+__device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNB / 2>& x,
+                                           int K, const Tail& tail, typename Op::Acc (&acc)[4][kNB], Late&& late) {
+  narrow_start<kNB>(lds, w, x, K, tail);
+  narrow_run<Op>(lds, w, x, K, tail, acc, late, [] {});
 }
 
 }  // namespace moe

@@ -18,6 +18,7 @@ namespace moe {
 
 constexpr int kThreads = 256;
 constexpr int kBandRows = 1024;  // rows of the tiles that take turns on one weight tile
+constexpr int kStaying = 256;    // workgroups of the whole tiles' kernel: one takes all of a compute unit's LDS
 constexpr int kDeal = 32;        // consecutive items that one XCD's compute units run at a time
 
 // A workgroup's tile: kW weight rows (features, or as many gate and up features in turn) by up to kX rows.
@@ -73,6 +74,7 @@ template <int kTile>
 struct Experts {
   int lo, hi;
   uint32_t end;
+  Experts() = default;
   __device__ __forceinline__ Experts(const Q8Args& a, int e0, const Before& b) {
     const int seen = b.seen;
     const int lane = threadIdx.x & 63, e = e0 + lane, rows = (int)a.rows;
@@ -98,64 +100,68 @@ struct Experts {
   }
 };
 
-// Workgroup b's item.  An expert's items are bands of kBandRows rows by all columns, the tiles of a band
-// next to each other; items are dealt to the XCDs (workgroups b, b + 8, ... share one) in runs of kDeal, so
-// that the compute units of an XCD read the same few weight and row tiles through its L2.  Every wave finds
-// the item by itself: 64 experts at a time, a lane each.
+// The items of a launch.  An expert's are bands of kBandRows rows by all columns, the tiles of a band next to
+// each other; they are dealt to the XCDs (workgroups b, b + 8, ... share one) in runs of kDeal, so that the
+// compute units of an XCD read the same few weight and row tiles through its L2.  Every wave finds an item by
+// itself, 64 experts at a time, a lane each.
 template <int kTile>
-__device__ __forceinline__ Item find_item(const Q8Args& a, uint32_t b, int cols) {
-  constexpr uint32_t kBand = kBandRows / kTile;
-  const uint32_t xcd = b % kXcds, j = b / kXcds;
-  // The item's number, of `total`.
-  auto dealt = [&](uint32_t total) {
+struct Items {
+  using X = Experts<kTile>;
+  X table;  // of up to 64 experts
+  uint32_t total = 0, cols;
+  __device__ __forceinline__ Items(const Q8Args& a, int cols_) : cols((uint32_t)cols_) {
+    if (!a.offsets) {
+      total = (uint32_t)((a.rows + kTile - 1) / kTile) * cols;
+    } else {
+      Before all;  // the tiles of all experts are counted first: the deal goes by their number
+      for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        table = X(a, e0, all);
+        all = table.after(a, e0);
+      }
+      total = all.tiles * cols;
+    }
+  }
+  // Item j of XCD xcd's.  It grows with j, so that an XCD without an item j has none after it.
+  __device__ __forceinline__ Item find(const Q8Args& a, uint32_t xcd, uint32_t j) const {
+    const Item none{0, 0, 0, 0};
+    if (total == 0) return none;
     const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
-    return ((j / run) * kXcds + xcd) * run + j % run;
-  };
-  auto item = [&](int expert, int lo, int hi, uint32_t tiles, uint32_t q) {
+    const uint32_t it = ((j / run) * kXcds + xcd) * run + j % run;
+    if (it >= total) return none;
+    if (!a.offsets) return place(0, 0, (int)a.rows, total / cols, it);
+    Item found = none;
+    if (a.experts <= 64) {
+      pick(table, 0, Before{}, it, found);
+      return found;
+    }
+    Before past;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+      const X x(a, e0, past);
+      if (pick(x, e0, past, it, found)) return found;
+      past = x.after(a, e0);
+    }
+    return none;
+  }
+
+ private:
+  // Item q of an expert with rows [lo, hi) in `tiles` tiles.
+  __device__ __forceinline__ Item place(int expert, int lo, int hi, uint32_t tiles, uint32_t q) const {
+    constexpr uint32_t kBand = kBandRows / kTile;
     const uint32_t band = q / (kBand * cols), in = q % (kBand * cols);
     const uint32_t nb = min(kBand, tiles - band * kBand);
     const int row0 = lo + (int)(band * kBand + in % nb) * kTile;
     return Item{expert, (int)(in / nb), min(kTile, hi - row0), row0};
-  };
-  using X = Experts<kTile>;
-  const Item none{0, 0, 0, 0};
-  if (!a.offsets) {
-    const uint32_t tiles = (uint32_t)((a.rows + kTile - 1) / kTile), it = dealt(tiles * cols);
-    return it < tiles * cols ? item(0, 0, (int)a.rows, tiles, it) : none;
   }
-  // The tiles of all experts are counted first: the deal goes by their number.
-  auto pick = [&](const X& x, int e0, const Before& b, uint32_t it, Item& found) {
+  __device__ __forceinline__ bool pick(const X& x, int e0, const Before& b, uint32_t it, Item& found) const {
     const uint64_t past = __ballot(it < x.end * cols);
     if (past == 0) return false;
     const int l = __builtin_ctzll(past);
     const uint32_t first = l == 0 ? b.tiles : (uint32_t)__builtin_amdgcn_readlane((int)x.end, l - 1);
     const uint32_t tiles = (uint32_t)__builtin_amdgcn_readlane((int)x.end, l) - first;
-    found = item(e0 + l, __builtin_amdgcn_readlane(x.lo, l), __builtin_amdgcn_readlane(x.hi, l), tiles, it - first * cols);
+    found = place(e0 + l, __builtin_amdgcn_readlane(x.lo, l), __builtin_amdgcn_readlane(x.hi, l), tiles, it - first * cols);
     return true;
-  };
-  Item found = none;
-  if (a.experts <= 64) {
-    const X x(a, 0, Before{});
-    const uint32_t total = x.after(a, 0).tiles * cols;
-    if (total == 0) return none;
-    const uint32_t it = dealt(total);
-    if (it < total) pick(x, 0, Before{}, it, found);
-    return found;
   }
-  Before all;
-  for (int e0 = 0; e0 < a.experts; e0 += 64) all = X(a, e0, all).after(a, e0);
-  const uint32_t total = all.tiles * cols;
-  if (total == 0) return none;
-  const uint32_t it = dealt(total);
-  if (it >= total) return none;
-  Before past;
-  for (int e0 = 0; e0 < a.experts; e0 += 64) {
-    const X x(a, e0, past);
-    if (pick(x, e0, past, it, found)) return found;
-    past = x.after(a, e0);
-  }
-  return none;
-}
+};
 
 // The item in scalar registers: it is the same in every lane.
 __device__ __forceinline__ Item uniform(const Item& it) {
@@ -252,21 +258,16 @@ __device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, DmaRows<kW 
 
 // One tile of kW weight rows by kX rows, of which it.rows are valid.
 template <bool gated, int kW, int kX>
-__device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t* lds) {
+__device__ __forceinline__ void small_item(const Q8Args& a, const Item& it, uint8_t* lds) {
   using S = Shape<gated, kW, kX>;
-  constexpr bool kNarrow = kW == 256 && kX <= 64;       // four waves by the weight rows alone
-  constexpr int kNI = kNarrow ? 4 : kW / 32;            // weight fragments per wave
-  constexpr int kNJ = kNarrow ? kX / 16 : kX / 32;      // row fragments per wave
-  constexpr int kDmaW = kW / 32, kDmaX = kX / 32;       // DMA instructions per wave and K step
+  constexpr int kNI = kW / 32, kNJ = kX / 32;      // fragments per wave of the weights and of the rows
+  constexpr int kDmaW = kW / 32, kDmaX = kX / 32;  // DMA instructions per wave and K step
   const int tid = item_thread(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lk = lane >> 4;
   const int K = a.K, N = a.N;
-  auto quad_n = [&](int i) {
-    return kNarrow ? (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16 + 4 * lk
-                   : (wave & 1) * (kW / 2) + i * 16 + 4 * lk;
-  };
-  auto quad_m = [&](int j) { return (kNarrow ? 0 : (wave >> 1) * (kX / 2)) + j * 16 + lr; };
+  auto quad_n = [&](int i) { return (wave & 1) * (kW / 2) + i * 16 + 4 * lk; };
+  auto quad_m = [&](int j) { return (wave >> 1) * (kX / 2) + j * 16 + lr; };
   const int first = it.col * S::kCols;
   auto feature = [&](int n) { return min(first + S::feature(n), N - 1); };
   const uint32_t r8 = (uint32_t)lane >> 3;
@@ -316,13 +317,7 @@ __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t
 
   i32x4 acc[kNI][kNJ];
   const ChunkTail tail(K);
-  auto nothing = [] {};
-  if constexpr (kNarrow)
-    narrow_mma<I8Mma, kNJ>(lds, w, x, K, tail, acc, nothing);
-  else if constexpr (kW == 256)
-    tile_mma<I8Mma, kNJ>(lds, w, x, K, tail, acc, nothing);
-  else
-    small_mma<kW, kX>(lds, w, x, K, tail, acc);
+  small_mma<kW, kX>(lds, w, x, K, tail, acc);
 
   float* scales = (float*)(lds + S::kScales);
   if (tid < kW) scales[tid] = my_ws;
@@ -362,32 +357,221 @@ __device__ __forceinline__ void q8_item(const Q8Args& a, const Item& it, uint8_t
   }
 }
 
-template <bool gated>
-__global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(Q8Args a, int cols) {
-  static_assert(Shape<gated, 256, 256>::kOutBytes <= kLdsBytes, "staged tile");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
-  const Item it = uniform(find_item<256>(a, blockIdx.x, cols));
-  const int rows = it.rows;
-  if (rows <= 0) return;
-  if (rows <= 32)
-    q8_item<gated, 256, 32>(a, it, lds);
-  else if (rows <= 64)
-    q8_item<gated, 256, 64>(a, it, lds);
-  else if (rows <= 128)
-    q8_item<gated, 256, 128>(a, it, lds);
-  else if (rows <= 192)
-    q8_item<gated, 256, 192>(a, it, lds);
-  else
-    q8_item<gated, 256, 256>(a, it, lds);
-}
-
 template <bool gated, int kW, int kX>
 __global__ __launch_bounds__(kThreads, kW + kX <= 128 ? 2 : 1) void q8_small_kernel(Q8Args a, int cols) {
   constexpr int kRing = 4 * (kW + kX) * kRowBytes, kOut = Shape<gated, kW, kX>::kOutBytes;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing > kOut ? kRing : kOut];
-  const Item it = uniform(find_item<kX>(a, blockIdx.x, cols));
+  const Item it = uniform(Items<kX>(a, cols).find(a, blockIdx.x % kXcds, blockIdx.x / kXcds));
   if (it.rows <= 0) return;
-  q8_item<gated, kW, kX>(a, it, lds);
+  small_item<gated, kW, kX>(a, it, lds);
+}
+
+// ------------------------------------------------------------------------------------ whole tiles
+
+// An accumulator's word.  As assembly: left to itself the compiler copies whole accumulators to vector registers
+// ahead of their use, and spills.
+__device__ __forceinline__ int acc_read(int v) {
+  int r;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(v));
+  return r;
+}
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// DMA instructions per wave and K step that a tile's rows take: it computes 32, 64, 128, 192 or 256 of them.
+__device__ __forceinline__ int row_dmas(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : rows <= 192 ? 6 : 8; }
+
+// What a tile's DMAs read.
+template <bool gated>
+struct TileSource {
+  using S = Shape<gated, 256, 256>;
+  DmaRows<kDmaPerThread> w;
+  DmaRows<8> x;
+  // First the rows, which may have to be looked up ...
+  __device__ __forceinline__ void rows(const Q8Args& a, const Item& it) {
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const int dx = row_dmas(it.rows);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int n = (wave * dx + i) * kRowsPerDma + (lane >> 3), m = it.row0 + min(n, it.rows - 1);
+      x.off[i] = (uint32_t)(a.index ? a.index[m] : m);
+    }
+  }
+  // ... then the addresses.  A row that row_index does not name takes row 0 (any readable one).
+  __device__ __forceinline__ void addresses(const Q8Args& a, const Item& it) {
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const int K = a.K, N = a.N, dx = row_dmas(it.rows), cmax = min(K / 16, 8) - 1;
+    const uint32_t r8 = (uint32_t)lane >> 3;
+    auto chunk = [&](uint32_t n) { return min(((uint32_t)lane & 7) ^ swz(n), (uint32_t)cmax) << 4; };
+    auto feature = [&](int n) { return min(it.col * S::kCols + S::feature(n), N - 1); };
+    w.step = x.step = kRowBytes;
+    const int f0 = feature(wave * 64);
+    w.base = (const uint8_t*)(S::up(wave * 64) ? a.w3 : a.w) + ((int64_t)it.expert * N + f0) * K;
+#pragma unroll
+    for (int i = 0; i < kDmaPerThread; ++i) {
+      const uint32_t n = (uint32_t)(wave * 64 + 8 * i) + r8;
+      w.off[i] = (uint32_t)(feature((int)n) - f0) * (uint32_t)K + chunk(n);
+    }
+    const int row0 = a.index ? 0 : it.row0;
+    x.base = a.x_rows > 0 ? (const uint8_t*)a.x + (int64_t)row0 * K : (const uint8_t*)a.w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t r = x.off[i];
+      x.off[i] = ((int64_t)r < a.x_rows ? (r - (uint32_t)row0) * (uint32_t)K : 0u) + chunk((uint32_t)(wave * dx + i) * kRowsPerDma + r8);
+      asm volatile("" ::"v"(x.off[i]));  // complete before the first DMA, which the compiler does not count
+    }
+  }
+  template <int kDma>
+  __device__ __forceinline__ DmaRows<kDma> first_rows() const {
+    DmaRows<kDma> r{x.base, x.step, {}};
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) r.off[i] = x.off[i];
+    return r;
+  }
+  // The first K steps on their way, the bases at the step after them.
+  __device__ __forceinline__ void start(const Q8Args& a, const Item& it, uint8_t* lds) {
+    const ChunkTail tail(a.K);
+    auto narrow = [&](auto dma) {
+      auto r = first_rows<decltype(dma)::value>();
+      narrow_start<2 * decltype(dma)::value>(lds, w, r, a.K, tail);
+      x.base = r.base;
+    };
+    auto tall = [&](auto dma) {
+      auto r = first_rows<decltype(dma)::value>();
+      tile_start<decltype(dma)::value>(lds, w, r, a.K, tail);
+      x.base = r.base;
+    };
+    using std::integral_constant;
+    switch (row_dmas(it.rows)) {
+      case 1: return narrow(integral_constant<int, 1>{});
+      case 2: return narrow(integral_constant<int, 2>{});
+      case 4: return tall(integral_constant<int, 4>{});
+      case 6: return tall(integral_constant<int, 6>{});
+      default: return tall(integral_constant<int, 8>{});
+    }
+  }
+};
+
+// The K loop and the epilogue of a tile of 32 kDma rows by 256 weight rows, whose first K steps `src` has started.
+// Between the two the next item's are started, so that they arrive under the epilogue: it keeps to registers,
+// where a staged tile would take the ring's LDS.
+template <bool gated, int kDma>
+__device__ __forceinline__ void tile_item(const Q8Args& a, const Item& it, const Item& next, TileSource<gated>& src, uint8_t* lds) {
+  using S = Shape<gated, 256, 256>;
+  constexpr bool kNarrow = kDma <= 2;              // four waves by the weight rows alone
+  constexpr int kNI = kNarrow ? 4 : 8;             // weight fragments per wave
+  constexpr int kNJ = kNarrow ? 2 * kDma : kDma;   // row fragments per wave
+  constexpr int kQuads = gated ? kNI / 2 : kNI;    // of them outputs
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  const int N = a.N;
+  // The lane is asked for anew in each part (item_thread), or what follows from it would stay in registers
+  // through the K loop.
+  auto quad_n = [&](int i) {
+    return kNarrow ? (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16 : (wave & 1) * 128 + i * 16;
+  };
+  auto quad_m = [&](int j, int lane) { return (kNarrow ? 0 : (wave >> 1) * (16 * kNJ)) + j * 16 + (lane & 15); };
+  const int first = it.col * S::kCols;
+  DmaRows<kDma> x = src.template first_rows<kDma>();
+  i32x4 acc[kNI][kNJ];
+  const ChunkTail tail(a.K);
+  // The scales and the next item's rows are asked for near the loop's end, the row scales (a load that may hang on
+  // another) in its last step: all are there when the loop ends, and no wait for them meets a DMA.
+  f32x4_any ws[kQuads], ws3[kQuads];
+  int r[kNJ];
+  float xs[kNJ];
+  auto late = [&] {
+    const int lane = item_thread() & 63;
+#pragma unroll
+    for (int i = 0; i < kQuads; ++i) {
+      const int64_t f = (int64_t)it.expert * N + min(first + S::feature(quad_n(i)) + 4 * (lane >> 4), N - 4);
+      ws[i] = *(const f32x4_any*)(a.ws + f);
+      if constexpr (gated) ws3[i] = *(const f32x4_any*)(a.ws3 + f);
+    }
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      const int m = it.row0 + min(quad_m(j, lane), it.rows - 1);
+      r[j] = a.index ? a.index[m] : m;
+    }
+    if (next.rows > 0) src.rows(a, next);
+  };
+  auto last = [&] {
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      xs[j] = __uint_as_float(0x7FC00000u);
+      if (r[j] >= 0 && r[j] < a.x_rows) xs[j] = a.xs[r[j]];
+    }
+  };
+  if constexpr (kNarrow)
+    narrow_run<I8Mma>(lds, src.w, x, a.K, tail, acc, late, last);
+  else
+    tile_run<I8Mma>(lds, src.w, x, a.K, tail, acc, late, last);
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) asm volatile("" ::"v"(xs[j]));
+#pragma unroll
+  for (int i = 0; i < kQuads; ++i) {
+    asm volatile("" ::"v"(ws[i]));
+    if constexpr (gated) asm volatile("" ::"v"(ws3[i]));
+  }
+  if (next.rows > 0) {
+    src.addresses(a, next);
+    src.start(a, next, lds);
+  }
+  const int lane = item_thread() & 63, lk = lane >> 4;
+  // A lane has 4 consecutive features of a row in each of two fragments; the lanes 16 apart exchange quads, so that
+  // each stores 8 consecutive features of one.
+#pragma unroll
+  for (int i = 0; i < kQuads; i += 2) {
+    const int f = first + S::feature(quad_n(i)) + (lk & 1) * 16 + (lk >> 1) * 8;
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      uint32_t h[2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = (float)acc_read(acc[i + u][j][q]) * (xs[j] * ws[i + u][q]);
+          if constexpr (gated) v[q] = silu_mul(v[q], (float)acc_read(acc[i + u + kNI / 2][j][q]) * (xs[j] * ws3[i + u][q]));
+        }
+        h[u][0] = bf16x2_of(v[0], v[1]);
+        h[u][1] = bf16x2_of(v[2], v[3]);
+      }
+      const auto lo = __builtin_amdgcn_permlane16_swap(h[0][0], h[1][0], false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(h[0][1], h[1][1], false, false);
+      const int m = quad_m(j, lane);
+      if (m < it.rows && f < N) *(u32x4*)(a.out + (int64_t)(it.row0 + m) * N + f) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
+    }
+  }
+}
+
+// Workgroups that stay: b takes item (b / 8 + 7 n) mod (workgroups of its XCD) of the n-th set that its XCD's
+// workgroups take together.  (Rotating keeps a workgroup from meeting the short last tile of one expert after
+// another.)
+template <bool gated>
+__global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(Q8Args a, int cols) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
+  const Items<256> items(a, cols);
+  const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, set = gridDim.x / kXcds;
+  uint32_t n = 0;
+  Item it = uniform(items.find(a, xcd, mine));
+  if (it.rows <= 0) return;
+  TileSource<gated> src;
+  src.rows(a, it);
+  src.addresses(a, it);
+  src.start(a, it, lds);
+  while (it.rows > 0) {
+    ++n;
+    const Item next = uniform(items.find(a, xcd, n * set + (mine + 7 * n) % set));
+    switch (row_dmas(it.rows)) {
+      case 1: tile_item<gated, 1>(a, it, next, src, lds); break;
+      case 2: tile_item<gated, 2>(a, it, next, src, lds); break;
+      case 4: tile_item<gated, 4>(a, it, next, src, lds); break;
+      case 6: tile_item<gated, 6>(a, it, next, src, lds); break;
+      default: tile_item<gated, 8>(a, it, next, src, lds); break;
+    }
+    it = next;
+  }
 }
 
 // ------------------------------------------------------------------------------------ few rows
@@ -553,7 +737,7 @@ hipError_t launch_tiles(const Q8Args& a, hipStream_t s) {
   const int64_t grid = (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   if constexpr (kW == 256)
-    hipLaunchKernelGGL(q8_tile_kernel<gated>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
+    hipLaunchKernelGGL(q8_tile_kernel<gated>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
   else
     hipLaunchKernelGGL((q8_small_kernel<gated, kW, kX>), dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
   return hipGetLastError();
