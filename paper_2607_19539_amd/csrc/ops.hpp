@@ -92,6 +92,7 @@ hipError_t launch_group(const GroupArgs& a, hipStream_t s);
 // matrix), or tiles of 64, 128 or 256 weight rows and as many rows through LDS.
 enum Q8Kind { kQ8Slim1, kQ8Slim2, kQ8Tiles64, kQ8Tiles128, kQ8Tiles256 };
 Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated);
+hipError_t launch_q8_kind(Q8Kind kind, const Q8Args& a, bool gated, hipStream_t s);
 hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s);
 
 }  // namespace moe

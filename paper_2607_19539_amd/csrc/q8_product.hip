@@ -37,10 +37,16 @@ struct Shape {
   static __device__ __forceinline__ bool up(int n) { return gated && (n / (kW / 4)) & 1; }
 };
 
-// silu(g) * u with the hardware exponential and reciprocal, each within about one fp32 ulp (the bf16
-// rounding that follows is 2^-9); a large negative g gives e^-g = inf, a reciprocal of 0 and a result of 0.
+// silu(g) * u = g u / (1 + e^-g) with the hardware's exponential and reciprocal, each within one fp32 ulp.  The
+// exponent -g log2(e) is rounded, which would cost e^-g an error of |g| 2^-24; the rounding is made good in the
+// first order (e (1 + r ln 2), four instructions), as a bf16 result that falls the other way may change the row's
+// 8-bit scale after it.  A large negative g gives e^-g = inf, a reciprocal of 0 and a result of 0.
 __device__ __forceinline__ float silu_mul(float g, float u) {
-  return (g * u) * __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+  constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147181f;
+  const float t = -g * kLog2e;
+  const float r = fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -t));
+  const float e = __builtin_amdgcn_exp2f(fminf(t, 127.0f));
+  return (g * u) * __builtin_amdgcn_rcpf(1.0f + fmaf(e, r * kLn2, e));
 }
 
 struct Item {
@@ -772,20 +778,24 @@ Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N
   return best;
 }
 
-hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s) {
-  switch (q8_kind(a.rows, a.offsets != nullptr, a.experts, a.K, a.N, gated)) {
+hipError_t launch_q8_kind(Q8Kind kind, const Q8Args& a, bool gated, hipStream_t s) {
+  switch (kind) {
     case kQ8Slim1:
       return gated ? launch_slim<true, 1>(a, s) : launch_slim<false, 1>(a, s);
-    case kQ8Slim2:
-      return launch_slim<false, 2>(a, s);
+    case kQ8Slim2:  // gated products have 16 features of each matrix in the other one
+      return gated ? launch_slim<true, 1>(a, s) : launch_slim<false, 2>(a, s);
     case kQ8Tiles64:
       return gated ? launch_tiles<true, 64, 64>(a, s) : launch_tiles<false, 64, 64>(a, s);
     case kQ8Tiles128:
       return gated ? launch_tiles<true, 128, 128>(a, s) : launch_tiles<false, 128, 128>(a, s);
     case kQ8Tiles256:
-      break;
+      return gated ? launch_tiles<true, 256, 256>(a, s) : launch_tiles<false, 256, 256>(a, s);
   }
-  return gated ? launch_tiles<true, 256, 256>(a, s) : launch_tiles<false, 256, 256>(a, s);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s) {
+  return launch_q8_kind(q8_kind(a.rows, a.offsets != nullptr, a.experts, a.K, a.N, gated), a, gated, s);
 }
 
 }  // namespace moe

@@ -4,6 +4,8 @@ The integer sums are exact, so a product differs from the definition by the roun
 two scales' product and of their product (3 units of 2^-24), and by the rounding to bf16 (2^-8).  The gated
 activation adds an exponential of g, whose error grows with |g|, below 2^-16 for |g| up to 60.
 """
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -170,3 +172,74 @@ def test_rows_of_a_large_tensor():
     out = torch.zeros((rows, 8), dtype=torch.bfloat16, device="cuda")
     B.moe_q8_product(x, torch.ones(rows, device="cuda"), w, torch.ones((1, 8), device="cuda"), out)
     assert bool((out[rows - 1] == 4096).all()) and float(out[:rows - 1].abs().max()) == 0.0
+
+
+KINDS = ["slim1", "slim2", "tiles64", "tiles128", "tiles256"]
+
+
+class Q8Args(ctypes.Structure):
+    """The launchers' arguments (csrc/ops.hpp)."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "xs", "index", "offsets", "w", "w3", "ws", "ws3", "out")] + \
+               [("x_rows", ctypes.c_int64), ("rows", ctypes.c_int64), ("experts", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("N", ctypes.c_int32)]
+
+
+def run_kind(kind, x, xs, w, ws, off, index, rows, gated):
+    """One of the kernels that launch_q8 chooses among, whatever it would choose."""
+    launch = B.load()._ZN3moe14launch_q8_kindENS_6Q8KindERKNS_6Q8ArgsEbP12ihipStream_t
+    launch.argtypes, launch.restype = [ctypes.c_int, ctypes.POINTER(Q8Args), ctypes.c_bool, ctypes.c_void_p], ctypes.c_int
+    t = [None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+         for a in (x, xs, index, off, w[0], w[1], ws[0], ws[1])]
+    out = torch.full((rows, w.shape[2]), SENTINEL, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    args = Q8Args(*[None if a is None else a.data_ptr() for a in t], out.data_ptr(), x.shape[0], rows, w.shape[1],
+                  x.shape[1], w.shape[2])
+    assert launch(KINDS.index(kind), ctypes.byref(args), gated, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy().astype(np.float64)
+
+
+# Rows of each expert (or of one matrix), K, N: every height of the whole tiles, several sets of items for each of
+# their workgroups, more experts than a wave has lanes; K of one chunk, of one step, of a few, with every kind of end.
+SIZES = [
+    (1, 16, 8), (300, 48, 72), (257, 112, 256), (520, 128, 264), (65, 144, 520), (193, 256, 136), (700, 272, 1032),
+    (260, 384, 40), (129, 400, 264), (64, 640, 520), (33, 1936, 264),
+    ([0, 5, 0, 0, 17, 1, 0], 64, 72), ([3, 64, 65, 128, 129, 31, 192, 193, 256, 257, 0, 1], 176, 520),
+    ([1300, 700, 2000, 0, 1096, 33, 64, 65, 128, 129, 1, 192, 193, 256, 257, 600], 272, 3080),
+    ([i % 5 for i in range(200)], 80, 136), ([i * 37 % 290 for i in range(130)], 144, 520),
+]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("counts,K,N", SIZES, ids=lambda v: str(v)[:24])
+def test_each_kernel(counts, K, N, kind, gather, gated):
+    log(f"q8 {kind} {str(counts)[:60]} K={K} N={N} gather={gather} gated={gated}")
+    rng = np.random.default_rng(K + N + gather)
+    grouped = not isinstance(counts, int)
+    c = counts if grouped else [counts]
+    off = np.concatenate([[0], np.cumsum(c)]).astype(np.int32)
+    rows = int(off[-1]) + (5 if grouped else 0)
+    n = max(1, rows // 3) if gather else rows
+    x, xs, w, ws = make(rng, n, K, N, len(c))
+    index = None
+    if gather:
+        index = rng.integers(0, n, rows).astype(np.int32)
+        index[rows // 2] = -5
+        index[rows - 1] = n
+    o = off if grouped else None
+    check(run_kind(kind, x, xs, w, ws, o, index, rows, gated), reference(x, xs, w, ws, o, index, rows, gated))
+
+
+@pytest.mark.parametrize("rows,grouped,E,K,N,gated,kind", [
+    (1, False, 1, 4096, 4096, False, "slim1"), (8, False, 1, 7168, 1024, False, "slim1"),
+    (96, True, 64, 1408, 2048, False, "slim2"), (96, True, 64, 2048, 1408, True, "slim1"),
+    (300, False, 1, 2000, 3000, False, "tiles64"), (16, False, 1, 4096, 14336, False, "tiles64"),
+    (256, False, 1, 4096, 14336, False, "tiles128"), (1024, False, 1, 4096, 4096, False, "tiles128"),
+    (4096, False, 1, 4096, 4096, False, "tiles256"), (49152, True, 64, 2048, 1408, True, "tiles256"),
+    (8192, True, 8, 14336, 4096, False, "tiles256")])
+def test_the_kernel_chosen(rows, grouped, E, K, N, gated, kind):
+    f = B.load()._ZN3moe7q8_kindElbiiib
+    f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_bool] + [ctypes.c_int32] * 3 + [ctypes.c_bool], ctypes.c_int
+    assert KINDS[f(rows, grouped, E, K, N, gated)] == kind
