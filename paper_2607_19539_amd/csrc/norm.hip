@@ -40,15 +40,26 @@ __device__ __forceinline__ T row_reduce(T v, T* part, F&& f) {
   return v;
 }
 
-// Four floats within +-127 to four int8: adding 1.5 * 2^23 rounds to the nearest even whole number and leaves
-// it in the lowest bits.
-__device__ __forceinline__ uint32_t quantise4(float a, float b, float c, float d, float inv) {
-  constexpr float kMagic = 12582912.0f;
-  const uint32_t ua = __float_as_uint(__fadd_rn(__fmul_rn(a, inv), kMagic)), ub = __float_as_uint(__fadd_rn(__fmul_rn(b, inv), kMagic));
-  const uint32_t uc = __float_as_uint(__fadd_rn(__fmul_rn(c, inv), kMagic)), ud = __float_as_uint(__fadd_rn(__fmul_rn(d, inv), kMagic));
-  const uint32_t lo = __builtin_amdgcn_perm(ub, ua, 0x0C0C0400u), hi = __builtin_amdgcn_perm(ud, uc, 0x04000C0Cu);
-  return lo | hi;
-}
+// How a row's values become int8: rne(y 127 / amax).  The quotient is a product with 1 / amax and a correction by
+// its remainder, which gives the fp32 nearest to it: with a product alone, values that fall half way between two
+// steps (bf16 rows have many) go up or down as 1 / amax happens to be rounded.
+struct Quantiser {
+  float times, top, inv;
+  explicit __device__ __forceinline__ Quantiser(float amax) {
+    const float down = amax > 0x1p100f ? 0x1p-64f : 1.0f;  // or 127 y might overflow
+    times = 127.0f * down;
+    top = amax * down;
+    inv = 1.0f / top;
+  }
+  // The step in the lowest byte: adding 1.5 * 2^23 rounds to the nearest even whole number.
+  __device__ __forceinline__ uint32_t step(float y) const {
+    const float t = __fmul_rn(y, times), p = __fmul_rn(t, inv);
+    return __float_as_uint(__fadd_rn(fmaf(fmaf(-p, top, t), inv, p), 12582912.0f));
+  }
+  __device__ __forceinline__ uint32_t four(float a, float b, float c, float d) const {
+    return __builtin_amdgcn_perm(step(b), step(a), 0x0C0C0400u) | __builtin_amdgcn_perm(step(d), step(c), 0x04000C0Cu);
+  }
+};
 
 constexpr int row_threads(int lanes) { return std::max(lanes, 256); }
 
@@ -146,14 +157,14 @@ __global__ __launch_bounds__(row_threads(kLanes)) void norm_kernel(NormArgs a) {
   const float amax = __uint_as_float(top);
   const bool finite = top < 0x7F800000u;
   const bool zero = !finite || amax < kTinyRow;
-  const float inv = zero ? 0.0f : 127.0f / amax;
+  const Quantiser to8(zero ? 1.0f : amax);
   if (lane == 0) a.scale[row] = !finite ? __uint_as_float(0x7FC00000u) : zero ? 0.0f : amax / 127.0f;
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     const int v = lane + i * kLanes;
     float y[8];
     normed(i, y);
-    u32x2 q = {quantise4(y[0], y[1], y[2], y[3], inv), quantise4(y[4], y[5], y[6], y[7], inv)};
+    u32x2 q = {to8.four(y[0], y[1], y[2], y[3]), to8.four(y[4], y[5], y[6], y[7])};
     if (zero) q = u32x2{};
     if (v < nvec) ((u32x2*)(a.out_q + row * a.H))[v] = q;
   }
