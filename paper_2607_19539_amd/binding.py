@@ -442,20 +442,24 @@ def moe_combine(recv, slot, gate, out, bad_slots=None, stream=None) -> int:
 
 # ----------------------------------------------------------------------------- operators around the stage
 
-@functools.lru_cache(maxsize=None)
-def _dtypes():
-    """The tensor types that the operators' arguments may have, by what they hold."""
-    import torch
-    return {"bf16": (torch.bfloat16, torch.int16), "int8": (torch.int8,), "int32": (torch.int32,),
-            "float32": (torch.float32,), "bfloat16": (torch.bfloat16,), "logits": (torch.float32, torch.bfloat16)}
+_KINDS: Dict[str, tuple] = {}  # the tensor types that arguments may have, by what they hold
+
+
+def _kinds():
+    if not _KINDS:
+        import torch
+        _KINDS.update(bf16=(torch.bfloat16, torch.int16), int8=(torch.int8,), int32=(torch.int32,),
+                      float32=(torch.float32,), bfloat16=(torch.bfloat16,), logits=(torch.float32, torch.bfloat16))
+    return _KINDS
 
 
 def _want(name, t, shape, kind):
     """Device pointer of a contiguous device tensor of exactly this shape and kind ("bf16" also takes the
     int16 bit patterns)."""
-    if t.dtype in _dtypes()[kind] and t.shape == shape and t.is_cuda and t.is_contiguous():
+    kinds = _KINDS or _kinds()
+    if t.shape == shape and t.dtype in kinds[kind] and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
-    if t.dtype not in _dtypes()[kind] or tuple(t.shape) != tuple(shape):
+    if t.dtype not in kinds[kind] or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)} of {kind}, got {list(t.shape)} of {t.dtype}")
     raise ValueError(f"{name} must be a contiguous device tensor")
 
@@ -531,7 +535,7 @@ def _logits(cfg, logits):
     T, E = _rows_of("logits", logits)
     if E != cfg.experts:
         raise ValueError(f"logits must have experts = {cfg.experts} columns, got {E}")
-    kind = MOE_TYPE_BF16 if logits.dtype in _dtypes()["bfloat16"] else MOE_TYPE_F32
+    kind = MOE_TYPE_BF16 if logits.dtype in _kinds()["bfloat16"] else MOE_TYPE_F32
     return T, E, _want("logits", logits, (T, E), "logits"), kind
 
 

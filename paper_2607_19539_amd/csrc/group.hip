@@ -18,7 +18,8 @@ namespace moe {
 constexpr int kThreads = 1024;  // a thread for each expert there can be
 constexpr int kWaves = kThreads / 64;
 constexpr int64_t kOneEntries = 4096;
-constexpr int64_t kBlockEntries = 4096;
+constexpr int64_t kBlockEntries = 2048;
+constexpr int kAhead = 4;  // entries of a lane that are read together
 constexpr int64_t kMostBlocks = 128;  // each one reads the counts of all of them
 
 // Entries of a workgroup: a multiple of kThreads.
@@ -82,25 +83,43 @@ __global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a, int6
 // kOne: one workgroup, no counts.
 template <bool kOne>
 __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int64_t entries, int bits) {
-  extern __shared__ int cnt[];  // [kWaves][experts]
+  extern __shared__ int cnt[];  // [kWaves][experts], at least 2 * kThreads
   __shared__ int part[kWaves], total;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
   const int64_t first = blockIdx.x * entries + wave * (entries / kWaves), end = first + entries / kWaves;
   int before = 0, all = 0;  // thread e: entries of expert e in earlier workgroups, and in all
-  if (!kOne && tid < E) {
-    const int blocks = gridDim.x, me = blockIdx.x;
-#pragma unroll 8
-    for (int b = 0; b < blocks; ++b) {
-      const int v = (int)a.counts[(int64_t)b * E + tid];
-      all += v;
-      before += b < me ? v : 0;
+  if constexpr (!kOne) {
+    // kThreads / E threads read each expert's counts, every so-many-th workgroup's, so that the reads are a round
+    // trip or two; the sums meet in LDS.
+    const int blocks = gridDim.x, me = blockIdx.x, sharers = kThreads / E, share = tid / E, e = tid % E;
+    if (share < sharers) {
+#pragma unroll 16
+      for (int b = share; b < blocks; b += sharers) {
+        const int v = (int)a.counts[(int64_t)b * E + e];
+        all += v;
+        before += b < me ? v : 0;
+      }
+      cnt[tid] = all;
+      cnt[kThreads + tid] = before;
     }
+    __syncthreads();
+    all = before = 0;
+    if (tid < E)
+      for (int i = tid; i < sharers * E; i += E) {
+        all += cnt[i];
+        before += cnt[kThreads + i];
+      }
+    __syncthreads();
   }
   for (int i = tid; i < kWaves * E; i += kThreads) cnt[i] = 0;
   __syncthreads();
-  for (int64_t i = first + lane; i < end; i += 64) {
-    const uint32_t id = id_of(a, i);
-    if (id < (uint32_t)E) atomicAdd(&cnt[wave * E + id], 1);
+  for (int64_t i0 = first + lane; i0 - lane < end; i0 += 64 * kAhead) {
+    uint32_t ids[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ids[u] = i0 + 64 * u < end ? id_of(a, i0 + 64 * u) : E;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (ids[u] < (uint32_t)E) atomicAdd(&cnt[wave * E + ids[u]], 1);
   }
   __syncthreads();
   if (kOne && tid < E)
@@ -121,22 +140,30 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int6
   }
   if (tid == E - 1) total = upto;
   __syncthreads();
-  for (int64_t i = first + lane; i - lane < end && i - lane < a.n; i += 64) {
-    const uint32_t id = id_of(a, i);
-    const uint64_t m = same_id(id, bits);
-    const int below = rank_below(m);
-    int pos = -1;
-    if (id < (uint32_t)E) {
-      pos = cnt[wave * E + id] + below;
-      // Read by all of them, then raised by the first: a wave's LDS operations happen in their order.
-      __builtin_amdgcn_wave_barrier();
-      if (below == 0) cnt[wave * E + id] = pos + (int)__popcll(m);
-      __builtin_amdgcn_wave_barrier();
-      a.row_token[pos] = (int)((uint32_t)i / (uint32_t)a.k);
-    }
-    if (i < a.n) {
-      a.slot[i] = pos;
-      if (i >= total) a.row_token[i] = -1;
+  for (int64_t i0 = first + lane; i0 - lane < end && i0 - lane < a.n; i0 += 64 * kAhead) {
+    uint32_t ids[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ids[u] = i0 + 64 * u < end ? id_of(a, i0 + 64 * u) : E;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t i = i0 + 64 * u;
+      if (i - lane >= end) break;
+      const uint32_t id = ids[u];
+      const uint64_t m = same_id(id, bits);
+      const int below = rank_below(m);
+      int pos = -1;
+      if (id < (uint32_t)E) {
+        pos = cnt[wave * E + id] + below;
+        // Read by all of them, then raised by the first: a wave's LDS operations happen in their order.
+        __builtin_amdgcn_wave_barrier();
+        if (below == 0) cnt[wave * E + id] = pos + (int)__popcll(m);
+        __builtin_amdgcn_wave_barrier();
+        a.row_token[pos] = (int)((uint32_t)i / (uint32_t)a.k);
+      }
+      if (i < a.n) {
+        a.slot[i] = pos;
+        if (i >= total) a.row_token[i] = -1;
+      }
     }
   }
 }
@@ -145,7 +172,7 @@ hipError_t launch_group(const GroupArgs& a, hipStream_t s) {
   int bits = 1;  // of the numbers 0 .. experts
   while ((a.experts >> bits) != 0) ++bits;
   const int blocks = (int)group_blocks(a.n, a.experts);
-  const uint32_t lds = (uint32_t)(kWaves * a.experts * sizeof(int));
+  const uint32_t lds = (uint32_t)(std::max(kWaves * a.experts, 2 * kThreads) * sizeof(int));
   if (blocks == 0) {
     const int64_t entries = ((int64_t)a.n + kThreads - 1) / kThreads * kThreads;
     hipLaunchKernelGGL(group_place_kernel<true>, dim3(1), dim3(kThreads), lds, s, a, entries, bits);
