@@ -450,7 +450,7 @@ int moe_norm(const void* x, const void* residual, const void* weight, int64_t ro
  *   dweight = sum over rows of dy * h * r    (fp32, in a fixed order of rows)
  * dx [rows, hidden] bf16 is the gradient of x and of residual alike; dsum (optional) is the gradient
  * that reaches sum_out from elsewhere and may be dx itself.  `workspace` holds at least
- * moe_norm_backward_workspace(rows, hidden) bytes (16-byte aligned).
+ * moe_norm_backward_workspace(rows, hidden) bytes (16-byte aligned; 0 for few rows, then NULL will do).
  */
 int64_t moe_norm_backward_workspace(int64_t rows, int32_t hidden);
 int moe_norm_backward(const void* dy, const void* h, const void* weight, const float* rstd, const void* dsum,

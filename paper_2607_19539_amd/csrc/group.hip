@@ -67,17 +67,23 @@ __device__ __forceinline__ int scan(int v, int* part) {
 }
 
 __global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a, int64_t entries) {
-  extern __shared__ int cnt[];  // [experts]
-  const int E = a.experts;
-  for (int e = threadIdx.x; e < E; e += kThreads) cnt[e] = 0;
+  extern __shared__ int cnt[];  // [kWaves][experts]: with few experts all waves would meet at their counts
+  const int E = a.experts, tid = threadIdx.x, wave = tid >> 6;
+  for (int i = tid; i < kWaves * E; i += kThreads) cnt[i] = 0;
   __syncthreads();
   const int64_t first = blockIdx.x * entries;
-  for (int64_t i = first + threadIdx.x; i < first + entries; i += kThreads) {
+#pragma unroll 2
+  for (int64_t i = first + tid; i < first + entries; i += kThreads) {
     const uint32_t id = id_of(a, i);
-    if (id < (uint32_t)E) atomicAdd(&cnt[id], 1);
+    if (id < (uint32_t)E) atomicAdd(&cnt[wave * E + id], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kThreads) a.counts[(int64_t)blockIdx.x * E + e] = (uint32_t)cnt[e];
+  for (int e = tid; e < E; e += kThreads) {
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += cnt[w * E + e];
+    a.counts[(int64_t)blockIdx.x * E + e] = (uint32_t)sum;
+  }
 }
 
 // kOne: one workgroup, no counts.
@@ -89,9 +95,9 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int6
   const int64_t first = blockIdx.x * entries + wave * (entries / kWaves), end = first + entries / kWaves;
   int before = 0, all = 0;  // thread e: entries of expert e in earlier workgroups, and in all
   if constexpr (!kOne) {
-    // kThreads / E threads read each expert's counts, every so-many-th workgroup's, so that the reads are a round
-    // trip or two; the sums meet in LDS.
-    const int blocks = gridDim.x, me = blockIdx.x, sharers = kThreads / E, share = tid / E, e = tid % E;
+    // Up to 16 threads read each expert's counts, every so-many-th workgroup's, so that the reads are a round trip
+    // or two; the sums meet in LDS.
+    const int blocks = gridDim.x, me = blockIdx.x, sharers = min(kThreads / E, 16), share = tid / E, e = tid % E;
     if (share < sharers) {
 #pragma unroll 16
       for (int b = share; b < blocks; b += sharers) {
@@ -179,7 +185,7 @@ hipError_t launch_group(const GroupArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const int64_t entries = block_entries(a.n);
-  hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), (uint32_t)(a.experts * sizeof(int)), s, a, entries);
+  hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), lds, s, a, entries);
   if (hipError_t e = hipGetLastError()) return e;
   hipLaunchKernelGGL(group_place_kernel<false>, dim3(blocks), dim3(kThreads), lds, s, a, entries, bits);
   return hipGetLastError();

@@ -119,7 +119,8 @@ int moe_norm(const void* x, const void* residual, const void* weight, int64_t ro
 
 int64_t moe_norm_backward_workspace(int64_t rows, int32_t hidden) {
   if (rows <= 0 || hidden <= 0 || hidden > kMaxHidden) return 0;
-  return norm_backward_parts(rows, hidden) * hidden * (int64_t)sizeof(float);
+  const int64_t parts = norm_backward_parts(rows, hidden);
+  return parts > 1 ? parts * hidden * (int64_t)sizeof(float) : 0;
 }
 
 int moe_norm_backward(const void* dy, const void* h, const void* weight, const float* rstd, const void* dsum,

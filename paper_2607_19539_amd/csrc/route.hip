@@ -343,10 +343,11 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
 // fp32 arrays read or written in vectors beside the logits, `also` one of the logits' type.
 template <class F>
 void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
-  // Sixteen lanes to a token cost the least work in all (a reduction over them is four steps, and four tokens
-  // share each); 64 lanes have the shorter chain, for few tokens.
-  const bool narrow = a.experts <= 256 && a.k <= 16 && a.tokens > 2048;
-  const int run = narrow ? (a.experts + 15) / 16 : (a.experts + 63) / 64;
+  // Few lanes to a token cost the least work in all (a reduction over 16 is four steps, and four tokens share
+  // each); 64 lanes have the shorter chain, for few tokens.
+  const bool many = a.tokens > 2048;
+  const int lanes = many && a.experts <= 256 && a.k <= 16 ? 16 : many && a.experts <= 512 && a.k <= 32 ? 32 : 64;
+  const int run = (a.experts + lanes - 1) / lanes;
   const uintptr_t align = a.bf16 ? 8 : 16;
   const bool vec = run % 4 == 0 && a.experts % 4 == 0 && (((uintptr_t)a.logits | (uintptr_t)also) & (align - 1)) == 0 &&
                    ((uintptr_t)f32 & 15) == 0;
@@ -363,7 +364,9 @@ void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
     kind(lanes, per, std::false_type{});
   };
   auto pick = [&](auto lanes) {
-    if (run <= 1)
+    if constexpr (decltype(lanes)::value == 32)
+      return with(lanes, std::integral_constant<int, 16>{});  // more than 256 experts
+    else if (run <= 1)
       with(lanes, std::integral_constant<int, 1>{});
     else if (run <= 2)
       with(lanes, std::integral_constant<int, 2>{});
@@ -374,8 +377,10 @@ void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
     else
       with(lanes, std::integral_constant<int, 16>{});
   };
-  if (narrow)
+  if (lanes == 16)
     pick(std::integral_constant<int, 16>{});
+  else if (lanes == 32)
+    pick(std::integral_constant<int, 32>{});
   else
     pick(std::integral_constant<int, 64>{});
 }

@@ -228,3 +228,19 @@ def test_norm_rows_past_four_gigabytes():
     B.moe_q8_rows(x, q, s)
     assert bool((s[:T - 1] == 1.0 / 127.0).all()) and float(s[T - 1]) == np.float32(5.0) / np.float32(127.0)
     assert q[T - 1, :5].tolist() == [25, 25, 25, 127, 25] and bool((q[T - 2] == 127).all())
+
+
+@pytest.mark.parametrize("T,H", [(1, 64), (2, 20008), (16, 2048), (17, 2048), (8, 4096), (4, 8192), (2, 16384)])
+def test_norm_backward_of_few_rows_into_any_float(T, H):
+    """One or two turns of rows need no workspace; dweight may begin at any float."""
+    x, _, w = inputs(T, H, 11)
+    dy = bf16(np.random.default_rng(12), (T, H), 0.1)
+    h, rstd = torch.empty((T, H), dtype=torch.bfloat16, device="cuda"), torch.empty(T, device="cuda")
+    B.moe_norm(x.cuda(), w.cuda(), EPS, sum_out=h, rstd=rstd)
+    room = torch.full((H + 2,), -7.0, device="cuda")
+    dx = torch.empty_like(h)
+    B.moe_norm_backward(dy.cuda(), h, w.cuda(), rstd, dx, room[1:H + 1])
+    _, _, rw, mw = gradients64(dy, x, w, None)
+    got = room.cpu().double()
+    assert float(got[0]) == -7.0 and float(got[H + 1]) == -7.0
+    assert bool(((got[1:H + 1] - rw).abs() <= (F32 + T * 2.0 ** -24) * mw).all())

@@ -30,7 +30,7 @@ def pipeline(T, H, E, k, F):
     back = torch.empty((rows, F), dtype=bf, **d)
     cfg = B.make_route_config(E, k, score=B.MOE_SCORE_SIGMOID, groups=4, top_groups=3, group_best=2, scale=2.5)
     ws = torch.empty(max(16, B.load().moe_group_workspace(rows, E)), dtype=torch.uint8, **d)
-    nws = torch.empty(B.load().moe_norm_backward_workspace(T, H), dtype=torch.uint8, **d)
+    nws = torch.empty(max(16, B.load().moe_norm_backward_workspace(T, H)), dtype=torch.uint8, **d)
 
     def call():
         B.moe_norm(x, w, 1e-6, residual=res, sum_out=s, out=out, out_q=q, scale=sc, rstd=r)

@@ -44,11 +44,11 @@ def test_norm_refusals():
 def test_norm_backward_refusals():
     lib = B.load()
 
-    def call(dy=P, h=P, w=P, rstd=P, dsum=None, rows=4, hidden=64, dx=P, dw=P, ws=P, n=1 << 30):
+    def call(dy=P, h=P, w=P, rstd=P, dsum=None, rows=400, hidden=64, dx=P, dw=P, ws=P, n=1 << 30):
         return lib.moe_norm_backward(dy, h, w, rstd, dsum, rows, hidden, dx, dw, ws, n, None)
 
-    need = lib.moe_norm_backward_workspace(4, 64)
-    assert need > 0 and lib.moe_norm_backward_workspace(0, 64) == 0
+    need = lib.moe_norm_backward_workspace(400, 64)
+    assert need > 0 and lib.moe_norm_backward_workspace(0, 64) == 0 and lib.moe_norm_backward_workspace(1, 64) == 0
     assert call(n=need - 1) == B.MOE_ECAPACITY
     assert call(ws=None) == B.MOE_ECAPACITY
     assert call(hidden=60) == B.MOE_EUNSUPPORTED
