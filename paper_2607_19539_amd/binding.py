@@ -442,30 +442,48 @@ def moe_combine(recv, slot, gate, out, bad_slots=None, stream=None) -> int:
 
 # ----------------------------------------------------------------------------- operators around the stage
 
-_KINDS: Dict[str, tuple] = {}  # the tensor types that arguments may have, by what they hold
+# What a tensor argument may hold (tensor_args.cpp has the same numbers): bf16 or its int16 bit patterns, int8,
+# int32, fp32, bf16 alone, fp32 or bf16.
+_BITS16, _INT8, _INT32, _F32, _BF16, _LOGITS = range(6)
+_KIND_NAMES = ("bf16", "int8", "int32", "float32", "bfloat16", "float32 or bfloat16")
+ARGS_PATH = os.path.join(PKG, "_lib", "_moe_args.so")
 
 
-def _kinds():
-    if not _KINDS:
-        import torch
-        _KINDS.update(bf16=(torch.bfloat16, torch.int16), int8=(torch.int8,), int32=(torch.int32,),
-                      float32=(torch.float32,), bfloat16=(torch.bfloat16,), logits=(torch.float32, torch.bfloat16))
-    return _KINDS
-
-
-def _want(name, t, shape, kind):
-    """Device pointer of a contiguous device tensor of exactly this shape and kind ("bf16" also takes the
-    int16 bit patterns)."""
-    kinds = _KINDS or _kinds()
-    if t.shape == shape and t.dtype in kinds[kind] and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    if t.dtype not in kinds[kind] or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)} of {kind}, got {list(t.shape)} of {t.dtype}")
+def _refuse(name, t, shape, kind):
+    """Raises what is wrong with a tensor argument."""
+    if not hasattr(t, "data_ptr"):
+        raise ValueError(f"{name} must be a device tensor, got {type(t).__name__}")
+    dtypes = {_BITS16: ("bfloat16", "int16"), _INT8: ("int8",), _INT32: ("int32",), _F32: ("float32",),
+              _BF16: ("bfloat16",), _LOGITS: ("float32", "bfloat16")}[kind]
+    if str(t.dtype)[6:] not in dtypes or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} of {_KIND_NAMES[kind]}, got {list(t.shape)} of {t.dtype}")
     raise ValueError(f"{name} must be a contiguous device tensor")
 
 
+def _load_args():
+    global _want, _opt
+    if not os.path.exists(ARGS_PATH):
+        raise RuntimeError(f"extension not built: {ARGS_PATH} (run `python -m paper_2607_19539_amd.build`)")
+    import torch  # noqa: F401  (the extension uses its libraries)
+    import importlib.machinery
+    import importlib.util
+    loader = importlib.machinery.ExtensionFileLoader("_moe_args", ARGS_PATH)
+    mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_moe_args", loader))
+    loader.exec_module(mod)
+    mod.set_refuse(_refuse)
+    _want, _opt = mod.want, mod.opt
+
+
+def _want(name, t, shape, kind):
+    """Device pointer of a contiguous device tensor of exactly this shape and kind (ValueError otherwise)."""
+    _load_args()
+    return _want(name, t, shape, kind)
+
+
 def _opt(name, t, shape, kind):
-    return None if t is None else _want(name, t, shape, kind)
+    """The same of an optional argument: None for None."""
+    _load_args()
+    return _opt(name, t, shape, kind)
 
 
 def _rows_of(name, t):
@@ -494,9 +512,9 @@ def moe_norm(x, weight, eps, residual=None, sum_out=None, out=None, out_q=None, 
     """Root-mean-square norm of x (+ residual) [T, H] bf16 by weight [H] bf16: the sum in sum_out, the normed
     rows in out (bf16) or out_q and scale (int8, fp32 [T]), 1 / sqrt(mean square + eps) in rstd (fp32 [T])."""
     T, H = sh = _rows_of("x", x)
-    args = (_want("x", x, sh, "bf16"), _opt("residual", residual, sh, "bf16"), _want("weight", weight, (H,), "bf16"), T,
-            H, eps, _opt("sum_out", sum_out, sh, "bf16"), _opt("out", out, sh, "bf16"),
-            _opt("out_q", out_q, sh, "int8"), _opt("scale", scale, (T,), "float32"), _opt("rstd", rstd, (T,), "float32"))
+    args = (_want("x", x, sh, _BITS16), _opt("residual", residual, sh, _BITS16), _want("weight", weight, (H,), _BITS16), T,
+            H, eps, _opt("sum_out", sum_out, sh, _BITS16), _opt("out", out, sh, _BITS16),
+            _opt("out_q", out_q, sh, _INT8), _opt("scale", scale, (T,), _F32), _opt("rstd", rstd, (T,), _F32))
     return _check(load().moe_norm(*args, _stream_ptr(stream)))
 
 
@@ -504,9 +522,9 @@ def moe_norm_backward(dy, h, weight, rstd, dx, dweight, dsum=None, workspace=Non
     """Gradients of moe_norm: dx [T, H] bf16 and dweight [H] fp32 from dy [T, H], the forward call's sum_out
     ``h`` and rstd, and the gradient ``dsum`` that reaches sum_out from elsewhere."""
     T, H = sh = _rows_of("dy", dy)
-    args = (_want("dy", dy, sh, "bf16"), _want("h", h, sh, "bf16"), _want("weight", weight, (H,), "bf16"),
-            _want("rstd", rstd, (T,), "float32"), _opt("dsum", dsum, sh, "bf16"), T, H, _want("dx", dx, sh, "bf16"),
-            _want("dweight", dweight, (H,), "float32"))
+    args = (_want("dy", dy, sh, _BITS16), _want("h", h, sh, _BITS16), _want("weight", weight, (H,), _BITS16),
+            _want("rstd", rstd, (T,), _F32), _opt("dsum", dsum, sh, _BITS16), T, H, _want("dx", dx, sh, _BITS16),
+            _want("dweight", dweight, (H,), _F32))
     lib = load()
     ws, n = _workspace(workspace, lib.moe_norm_backward_workspace(T, H), stream)
     return _check(lib.moe_norm_backward(*args, ws if ws is None else ws.data_ptr(), n, _stream_ptr(stream)))
@@ -515,15 +533,15 @@ def moe_norm_backward(dy, h, weight, rstd, dx, dweight, dsum=None, workspace=Non
 def moe_q8_rows(x, q, scale, stream=None) -> int:
     """bf16 rows [T, H] to int8 with one fp32 scale each."""
     T, H = sh = _rows_of("x", x)
-    return _check(load().moe_q8_rows(_want("x", x, sh, "bf16"), T, H, _want("q", q, sh, "int8"),
-                                     _want("scale", scale, (T,), "float32"), _stream_ptr(stream)))
+    return _check(load().moe_q8_rows(_want("x", x, sh, _BITS16), T, H, _want("q", q, sh, _INT8),
+                                     _want("scale", scale, (T,), _F32), _stream_ptr(stream)))
 
 
 def moe_q8_restore(q, scale, out, stream=None) -> int:
     """int8 rows [T, H] and their scales back to bf16."""
     T, H = sh = _rows_of("q", q)
-    return _check(load().moe_q8_restore(_want("q", q, sh, "int8"), _want("scale", scale, (T,), "float32"), T, H,
-                                        _want("out", out, sh, "bf16"), _stream_ptr(stream)))
+    return _check(load().moe_q8_restore(_want("q", q, sh, _INT8), _want("scale", scale, (T,), _F32), T, H,
+                                        _want("out", out, sh, _BITS16), _stream_ptr(stream)))
 
 
 def make_route_config(experts, k, score=MOE_SCORE_SOFTMAX, groups=1, top_groups=1, group_best=1, renormalise=True,
@@ -535,24 +553,24 @@ def _logits(cfg, logits):
     T, E = _rows_of("logits", logits)
     if E != cfg.experts:
         raise ValueError(f"logits must have experts = {cfg.experts} columns, got {E}")
-    kind = MOE_TYPE_BF16 if logits.dtype in _kinds()["bfloat16"] else MOE_TYPE_F32
-    return T, E, _want("logits", logits, (T, E), "logits"), kind
+    kind = MOE_TYPE_BF16 if logits.element_size() == 2 else MOE_TYPE_F32
+    return T, E, _want("logits", logits, (T, E), _LOGITS), kind
 
 
 def moe_route(cfg: moe_route_config_t, logits, ids, weights, bias=None, scores=None, stream=None) -> int:
     """Chooses cfg.k experts for each token from logits [T, E] (fp32 or bf16): ids [T, k] int32, weights [T, k]
     fp32, and, where wanted, the scores [T, E] fp32.  ``bias`` [E] fp32 is added for the choice alone."""
     T, E, ptr, kind = _logits(cfg, logits)
-    args = (_opt("bias", bias, (E,), "float32"), T, _want("ids", ids, (T, cfg.k), "int32"),
-            _want("weights", weights, (T, cfg.k), "float32"), _opt("scores", scores, (T, E), "float32"))
+    args = (_opt("bias", bias, (E,), _F32), T, _want("ids", ids, (T, cfg.k), _INT32),
+            _want("weights", weights, (T, cfg.k), _F32), _opt("scores", scores, (T, E), _F32))
     return _check(load().moe_route(ctypes.byref(cfg), ptr, kind, *args, _stream_ptr(stream)))
 
 
 def moe_route_backward(cfg: moe_route_config_t, logits, ids, dweights, dlogits, dscores=None, stream=None) -> int:
     """Gradient of moe_route's weights (and scores) by the logits, in the logits' type."""
     T, E, ptr, kind = _logits(cfg, logits)
-    args = (_want("ids", ids, (T, cfg.k), "int32"), _want("dweights", dweights, (T, cfg.k), "float32"),
-            _opt("dscores", dscores, (T, E), "float32"), T, _want("dlogits", dlogits, (T, E), "bfloat16" if kind == MOE_TYPE_BF16 else "float32"))
+    args = (_want("ids", ids, (T, cfg.k), _INT32), _want("dweights", dweights, (T, cfg.k), _F32),
+            _opt("dscores", dscores, (T, E), _F32), T, _want("dlogits", dlogits, (T, E), _BF16 if kind == MOE_TYPE_BF16 else _F32))
     return _check(load().moe_route_backward(ctypes.byref(cfg), ptr, kind, *args, _stream_ptr(stream)))
 
 
@@ -560,8 +578,8 @@ def moe_group(ids, experts, expert_offsets, row_token, slot, workspace=None, str
     """Sorts the choices ids [T, k] int32 by expert: expert_offsets [E + 1], the token of each row in row_token
     [T * k] and the row of each choice in slot [T, k], all int32."""
     T, k = sh = _rows_of("ids", ids)
-    args = (_want("ids", ids, sh, "int32"), T, k, experts, _want("expert_offsets", expert_offsets, (experts + 1,), "int32"),
-            _want("row_token", row_token, (T * k,), "int32"), _want("slot", slot, sh, "int32"))
+    args = (_want("ids", ids, sh, _INT32), T, k, experts, _want("expert_offsets", expert_offsets, (experts + 1,), _INT32),
+            _want("row_token", row_token, (T * k,), _INT32), _want("slot", slot, sh, _INT32))
     lib = load()
     ws, n = _workspace(workspace, lib.moe_group_workspace(T * k, experts), stream)
     return _check(lib.moe_group(*args, ws if ws is None else ws.data_ptr(), n, _stream_ptr(stream)))
@@ -575,10 +593,10 @@ def _q8_operands(xq, x_scale, w, w_scale, out, row_index, expert_offsets, name="
         raise ValueError(f"xq must have at least out's {rows} rows, got {n}")
     if expert_offsets is None and E != 1:
         raise ValueError("expert_offsets is needed with more than one expert")
-    lead = (_want("xq", xq, (n, K), "int8"), _want("x_scale", x_scale, (n,), "float32"), n,
-            _opt("row_index", row_index, (rows,), "int32"), _opt("expert_offsets", expert_offsets, (E + 1,), "int32"), E)
-    mats = (_want(name, w, (E, N, K), "int8"), _want(name + "_scale", w_scale, (E, N), "float32"))
-    return lead, mats, (rows, K, N, _want("out", out, (rows, N), "bf16"))
+    lead = (_want("xq", xq, (n, K), _INT8), _want("x_scale", x_scale, (n,), _F32), n,
+            _opt("row_index", row_index, (rows,), _INT32), _opt("expert_offsets", expert_offsets, (E + 1,), _INT32), E)
+    mats = (_want(name, w, (E, N, K), _INT8), _want(name + "_scale", w_scale, (E, N), _F32))
+    return lead, mats, (rows, K, N, _want("out", out, (rows, N), _BITS16))
 
 
 def moe_q8_product(xq, x_scale, w, w_scale, out, row_index=None, expert_offsets=None, stream=None) -> int:
@@ -591,7 +609,7 @@ def moe_q8_product(xq, x_scale, w, w_scale, out, row_index=None, expert_offsets=
 def moe_q8_gated(xq, x_scale, w1, w1_scale, w3, w3_scale, out, row_index=None, expert_offsets=None, stream=None) -> int:
     """out [rows, N] bf16 = silu(g) * u of the two products g (w1) and u (w3) of the same rows."""
     lead, mats, tail = _q8_operands(xq, x_scale, w1, w1_scale, out, row_index, expert_offsets, "w1")
-    more = (_want("w3", w3, w1.shape, "int8"), _want("w3_scale", w3_scale, w1_scale.shape, "float32"))
+    more = (_want("w3", w3, w1.shape, _INT8), _want("w3_scale", w3_scale, w1_scale.shape, _F32))
     return _check(load().moe_q8_gated(*lead, *mats, *more, *tail, _stream_ptr(stream)))
 
 

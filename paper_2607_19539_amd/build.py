@@ -1,4 +1,5 @@
-"""Build the gfx950 shared library ``_lib/libmoe_stage.so`` with hipcc.
+"""Build the gfx950 shared library ``_lib/libmoe_stage.so`` with hipcc, and ``_lib/_moe_args.so``, the binding's
+check of tensor arguments, with the host compiler.
 
 Run as ``python -m paper_2607_19539_amd.build``.  Cross-compiles without a GPU.
 """
@@ -14,6 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libmoe_stage.so")
+ARGS_LIB = os.path.join(LIBDIR, "_moe_args.so")
 SOURCES = ["kernels.hip", "combine.hip", "plan_device.hip", "norm.hip", "route.hip", "group.hip", "q8_product.hip", "plan.cpp",
            "api.cpp", "ops_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -38,7 +40,23 @@ def build(verbose: bool = False) -> str:
         out_tmp = LIB + ".tmp"
         _run([HIPCC, *DEVICE_FLAGS, "-shared", "-fPIC", *objs, "-o", out_tmp], verbose)
         os.replace(out_tmp, LIB)
+    build_args(verbose)
     return LIB
+
+
+def build_args(verbose: bool = False) -> None:
+    """The Python extension tensor_args.cpp: host code against torch's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    includes = [sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{i}" for i in includes],
+          os.path.join(CSRC, "tensor_args.cpp"), "-o", ARGS_LIB + ".tmp", f"-L{lib}", "-ltorch_python", "-ltorch_cpu",
+          "-lc10", f"-Wl,-rpath,{lib}"], verbose)
+    os.replace(ARGS_LIB + ".tmp", ARGS_LIB)
 
 
 def _run(cmd, verbose):

@@ -156,7 +156,10 @@ def test_binding_checks_tensors():
     with pytest.raises(ValueError, match="device"):
         B.moe_norm(x, w, 1e-6, out=x)
     with pytest.raises(ValueError, match="weight"):
-        B._want("weight", w, (32,), "bf16")
+        B._want("weight", w, (32,), B._BITS16)
+    with pytest.raises(ValueError, match="got float"):
+        B._opt("weight", 1.5, (64,), B._BITS16)
+    assert B._opt("weight", None, (64,), B._BITS16) is None
     with pytest.raises(ValueError, match="two dimensions"):
         B.moe_norm(w, w, 1e-6, out=w)
     cfg = B.make_route_config(8, 2)
