@@ -131,12 +131,6 @@ __device__ __forceinline__ Softmax softmax_of(const Place<kLanes>& at, const flo
   return s;
 }
 
-// A float as an unsigned integer of the same order, above 0 (-0 counts as 0); 0 for -infinity.
-__device__ __forceinline__ uint32_t ordered(float f) {
-  const uint32_t u = __float_as_uint(f + 0.0f);
-  return f == -kInf ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
 // Leaves the picks of the token's best groups and makes the others -infinity.  A group of a whole power of
 // two of lanes is reduced in registers, another through the wave's LDS.
 template <int kLanes, int kPer>
@@ -212,6 +206,13 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, const Place<kLan
     if (!((keep >> ((at.e0 + i) / size & 63)) & 1)) pick[i] = -kInf;
 }
 
+// v of the token's lane `lane`; a whole wave's is the same in all of its lanes, and a scalar read.
+template <int kLanes>
+__device__ __forceinline__ int from_lane(int v, int lane) {
+  if constexpr (kLanes == 64) return __builtin_amdgcn_readlane(v, __builtin_amdgcn_readfirstlane(lane));
+  return __shfl(v, lane, kLanes);
+}
+
 template <int kLanes, int kPer, bool kVec, bool kSig>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   __shared__ float picks[kThreads / kLanes][kLanes * kPer];
@@ -239,27 +240,24 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   }
   const bool poisoned = at.mine(__ballot(nan)) != 0;
   if (a.groups > 1) keep_groups<kLanes, kPer>(a, at, pick, picks[threadIdx.x / kLanes]);
-  // One choice after another: the largest pick, the lowest expert among equals.
-  uint32_t left[kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) left[i] = ordered(pick[i]);
+  // One choice after another: the largest pick, the lowest expert among equals; -infinity is none.
   int id = -1;
   for (int j = 0; j < a.k; ++j) {
-    uint32_t best = left[0];
+    float best = pick[0];
 #pragma unroll
-    for (int i = 1; i < kPer; ++i) best = max(best, left[i]);
-    best = wave_reduce<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+    for (int i = 1; i < kPer; ++i) best = fmaxf(best, pick[i]);
+    best = wave_reduce<kLanes>(best, fmax2);
     // The first of the lane's experts with it; of several lanes' the first lane's, whose experts come first.
     int found = kPer;
 #pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) found = left[i] == best ? i : found;
-    const uint64_t who = best != 0 ? at.mine(__ballot(found < kPer)) : 0;
+    for (int i = kPer - 1; i >= 0; --i) found = pick[i] == best ? i : found;
+    const uint64_t who = at.mine(__ballot(found < kPer && best > -kInf));
     const int first = __builtin_ctzll(who | 1ull << 63);
-    const int e = __shfl(at.e0 + found, first, kLanes);
+    const int e = from_lane<kLanes>(at.e0 + found, first);
     if (at.lane == j && who != 0) id = e;
     if (at.lane != first) found = kPer;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) left[i] = found == i ? 0u : left[i];
+    for (int i = 0; i < kPer; ++i) pick[i] = found == i ? -kInf : pick[i];
   }
   const bool mine = at.have && at.lane < a.k;
   if (poisoned) id = at.lane;
