@@ -4,6 +4,18 @@
 //
 // v_mfma_i32_16x16x64_i8, 32-bit integer sums (exact).  The weights are the A operand, so a lane ends up with
 // 4 consecutive features of one row and stores them together.
+//
+// Three kinds of kernel, chosen by an estimate of each one's time (q8_kind):
+//  * whole tiles of 256 weight rows by up to 256 rows on the K loops of mma_tile.hpp, one workgroup a compute unit
+//    that stays and starts its next tile's loads under the epilogue.  The chip's power bounds them: 8192 rows by
+//    14336 x 4096 take 322 us (2.99 POP/s), 8192 x 8192 x 8192 384 (2.86; the library's product takes 542); a K step
+//    takes 1.5 us with random operands, whether they come from L2 or from memory, and 1.04 with zeros (4.1 POP/s).
+//    A tile costs some 8 us besides its K steps, which is a quarter of the time at K 2048.
+//  * tiles of 128 or 64, whose loads bound them, where whole tiles would leave compute units idle: 300 rows by 2000 x
+//    3000 8.1 us with tiles of 64, 27.5 with whole ones; 1024 by 4096 x 4096 23 with tiles of 128, 40.
+//  * 16 rows by 16 or 32 features straight from memory into registers, K divided among the waves, for a few rows of
+//    each expert: bound by the reading of the weights (32 experts of 7168 x 2048, 8 rows each: 470 MB in 83 us, 5.7
+//    TB/s) or, in small matrices, by its latency (one row by 4096 x 4096 5.9 us, 9.3 with tiles of 64).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -6,6 +6,10 @@
 //   gradient: dp_j = scale / P (dw_j - sum_i dw_i p_i / P) (+ dscores),
 //             softmax dl_e = p_e (dp_e - sum dp p),  sigmoid dl_e = dp_e p_e (1 - p_e)
 //
+// Many tokens are bound by vector instructions, not by memory: 32768 tokens of 256 experts take 25 us forward (1600
+// instructions for four tokens, half of them in the choice of 8; reading the logits alone would take 7) and 18 back
+// (67 MB, 3.7 TB/s).  A few are bound by the chain of the choices: 32 of 256 take 5 us.
+//
 // kLanes lanes take a token; lane i holds the experts i * run .. i * run + run - 1 (run <= kPer) in registers.
 // A score has to come out the same however it is computed, or near ties fall differently from one pass (or one
 // launch shape) to the next: expf and the division are the correctly specified ones, and the softmax's sum is
@@ -342,7 +346,8 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
 template <class F>
 void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
   // Few lanes to a token cost the least work in all (a reduction over 16 is four steps, and four tokens share
-  // each); 64 lanes have the shorter chain, for few tokens.
+  // each): 32768 tokens of 256 experts 25 us with 16 lanes, 69 with 64; 21082 of 384 and back 34 with 32 lanes, 43
+  // with 64.  64 lanes have the shorter chain, for few tokens.
   const bool many = a.tokens > 2048;
   const int lanes = many && a.experts <= 256 && a.k <= 16 ? 16 : many && a.experts <= 512 && a.k <= 32 ? 32 : 64;
   const int run = (a.experts + lanes - 1) / lanes;
