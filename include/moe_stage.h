@@ -426,6 +426,8 @@ int moe_combine(const void* recv, int64_t recv_rows, int32_t hidden, const int32
  * captured in a graph.  Unless said otherwise, outputs are written in full and
  * may not overlap an input.  16-bit tensors are bf16; they and the int8 ones are
  * 16-byte aligned, the others (the router's logits among them) to their element.
+ * A call whose rows or tokens need 2^32 threads or more is MOE_EUNSUPPORTED; a
+ * token has 16 to 64 of them, a row 64 to 1024.
  * ------------------------------------------------------------------------- */
 
 /*

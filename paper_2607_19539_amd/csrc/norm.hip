@@ -202,15 +202,18 @@ void by_row(int64_t rows, int32_t H, F&& f) {
 }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  bool fits = true;
   by_row(a.rows, a.H, [&](auto lanes, auto vecs) {
     constexpr int L = decltype(lanes)::value, V = decltype(vecs)::value, kRows = row_threads(L) / L;
-    const dim3 grid((uint32_t)((a.rows + kRows - 1) / kRows));
+    const int64_t blocks = (a.rows + kRows - 1) / kRows;
+    const dim3 grid((uint32_t)blocks);
+    if (!(fits = launch_fits(blocks, row_threads(L)))) return;
     if (a.weight)
       hipLaunchKernelGGL((norm_kernel<L, V, true>), grid, dim3(row_threads(L)), 0, s, a);
     else
       hipLaunchKernelGGL((norm_kernel<L, V, false>), grid, dim3(row_threads(L)), 0, s, a);
   });
-  return hipGetLastError();
+  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
 
 // ------------------------------------------------------------------------------------ gradients
@@ -433,10 +436,13 @@ __global__ __launch_bounds__(256) void restore_kernel(RestoreArgs a) {
 }
 
 hipError_t launch_restore(const RestoreArgs& a, hipStream_t s) {
-  if (a.H <= 2048)
-    hipLaunchKernelGGL(restore_kernel<64>, dim3((uint32_t)((a.rows + 3) / 4)), dim3(256), 0, s, a);
+  const bool wave = a.H <= 2048;
+  const int64_t blocks = wave ? (a.rows + 3) / 4 : a.rows;
+  if (!launch_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  if (wave)
+    hipLaunchKernelGGL(restore_kernel<64>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL(restore_kernel<256>, dim3((uint32_t)a.rows), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(restore_kernel<256>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -78,6 +78,9 @@ struct Q8Args {
   int32_t experts, K, N;
 };
 
+// A launch has fewer than 2^32 threads; one that would need more is refused with hipErrorInvalidConfiguration.
+constexpr bool launch_fits(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
+
 hipError_t launch_norm(const NormArgs& a, hipStream_t s);
 // Partial sums of the weight's gradient: rows of [H] floats in the workspace.
 int64_t norm_backward_parts(int64_t rows, int32_t H);

@@ -19,6 +19,7 @@ constexpr int32_t kMaxInFeatures = 131056;  // 2^17 - 16: |sum| of products of u
 bool misaligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
 
 int launched(hipError_t e, const char* who) {
+  if (e == hipErrorInvalidConfiguration) return record_error(MOE_EUNSUPPORTED, who, "more rows than one launch takes");
   return e == hipSuccess ? MOE_OK : record_error(MOE_EHIP, who, hipGetErrorString(e));
 }
 

@@ -739,21 +739,31 @@ __global__ __launch_bounds__(kThreads) void q8_slim_kernel(Q8Args a) {
   }
 }
 
+// Tiles of `height` rows there can be: every expert may end in a partly filled one.
+int64_t most_tiles(int64_t rows, bool grouped, int32_t experts, int height) {
+  return (rows + height - 1) / height + (grouped ? std::min<int64_t>(experts, rows) : 0);
+}
+
+constexpr int64_t kSlimTiles = 65535;  // they are the grid's second axis
+
+int64_t dealt(int64_t tiles, int cols) {
+  return (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
+}
+
 template <bool gated, int kN>
 hipError_t launch_slim(const Q8Args& a, hipStream_t s) {
-  const int64_t tiles = (a.rows + 15) / 16 + (a.offsets ? std::min<int64_t>(a.experts, a.rows) : 0);
-  if (tiles > 65535) return hipErrorInvalidConfiguration;
+  const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, 16);
+  if (tiles > kSlimTiles) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((q8_slim_kernel<gated, kN, 1>), dim3((a.N + 16 * kN - 1) / (16 * kN), (uint32_t)tiles), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 template <bool gated, int kW, int kX>
 hipError_t launch_tiles(const Q8Args& a, hipStream_t s) {
-  // Tiles there can be: every expert may end in a partly filled one.
-  const int64_t tiles = (a.rows + kX - 1) / kX + (a.offsets ? std::min<int64_t>(a.experts, a.rows) : 0);
+  const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, kX);
   const int cols = (a.N + Shape<gated, kW, kX>::kCols - 1) / Shape<gated, kW, kX>::kCols;
-  const int64_t grid = (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  const int64_t grid = dealt(tiles, cols);
+  if (kW == 256 ? grid > INT32_MAX : !launch_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   if constexpr (kW == 256)
     hipLaunchKernelGGL(q8_tile_kernel<gated>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
   else
@@ -780,9 +790,13 @@ Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N
   auto consider = [&](Q8Kind kind, double c) {
     if (c < least) best = kind, least = c;
   };
-  consider(kQ8Tiles128, cost(2 + std::ceil(half) * (nk * 0.61 + 1), 4.6));
-  consider(kQ8Tiles64, cost(3 + std::max(1.0, quarter) * (nk * 0.2 + 0.3), 5.2));
-  if (tiles(16) <= 65535) {
+  // The small tiles and the slim kernels have a workgroup for each item, and can be too many for one launch.
+  auto launches = [&](int w, int x) {
+    return launch_fits(dealt(most_tiles(rows, grouped, experts, x), (int)std::ceil(features / w)), kThreads);
+  };
+  if (launches(128, 128)) consider(kQ8Tiles128, cost(2 + std::ceil(half) * (nk * 0.61 + 1), 4.6));
+  if (launches(64, 64)) consider(kQ8Tiles64, cost(3 + std::max(1.0, quarter) * (nk * 0.2 + 0.3), 5.2));
+  if (most_tiles(rows, grouped, experts, 16) <= kSlimTiles) {
     const double slim = items(gated ? 32 : 16, 16), slim2 = items(32, 16);
     consider(kQ8Slim1, cost(2 + nk * std::max(0.1, (gated ? 0.14 : 0.12) * slim), 5.8));
     if (!gated) consider(kQ8Slim2, cost(2 + nk * std::max(0.16, 0.16 * slim2), 5.8));

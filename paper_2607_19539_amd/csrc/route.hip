@@ -388,25 +388,31 @@ void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
     pick(std::integral_constant<int, 64>{});
 }
 
-dim3 token_grid(const RouteArgs& a, int lanes) {
+int64_t token_blocks(const RouteArgs& a, int lanes) {
   const int64_t per = kThreads / lanes;
-  return dim3((uint32_t)((a.tokens + per - 1) / per));
+  return (a.tokens + per - 1) / per;
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
+  bool fits = true;
   by_shape(a, nullptr, a.bias, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
-    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
+    const int64_t blocks = token_blocks(a, L);
+    if (!(fits = launch_fits(blocks, kThreads))) return;
+    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
   });
-  return hipGetLastError();
+  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
 
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s) {
+  bool fits = true;
   by_shape(a, a.dlogits, a.dscores, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
-    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), token_grid(a, L), dim3(kThreads), 0, s, a);
+    const int64_t blocks = token_blocks(a, L);
+    if (!(fits = launch_fits(blocks, kThreads))) return;
+    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
   });
-  return hipGetLastError();
+  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
 }
 
 }  // namespace moe

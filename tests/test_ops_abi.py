@@ -149,6 +149,36 @@ def test_q8_product_refusals(gated):
     assert ("moe_q8_gated" if gated else "moe_q8_product") in B.moe_stage_last_error(None)
 
 
+def test_more_rows_than_a_launch_takes():
+    """A launch has fewer than 2^32 threads, of which a row or a token has a share."""
+    lib, cfg = B.load(), B.make_route_config(8, 2)
+    most = 2 ** 31 - 1
+    assert lib.moe_q8_rows(P, most, 4096, P, P, None) == B.MOE_EUNSUPPORTED
+    assert "rows" in B.moe_stage_last_error(None)
+    assert norm(rows=most, hidden=65536) == B.MOE_EUNSUPPORTED
+    assert lib.moe_q8_restore(P, P, most, 4096, P, None) == B.MOE_EUNSUPPORTED
+    assert lib.moe_route(cfg, P, B.MOE_TYPE_F32, None, most, P, P, None, None) == B.MOE_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,grouped,E,K,N", [
+    (1048000, True, 1024, 16, 8), (1048000, True, 8, 16, 8), (1048560, False, 1, 16, 8), (1048561, False, 1, 16, 8),
+    (1040000, True, 1024, 128, 64), (2 ** 31 - 1, False, 1, 16, 8), (2 ** 31 - 1, True, 1024, 16, 8),
+    (2 ** 30, False, 1, 128, 64)])
+def test_the_product_chosen_can_be_launched(rows, grouped, E, K, N, gated):
+    """No choice whose workgroups are more than a launch takes, at sizes where the estimates prefer the small ones."""
+    f = B.load()._ZN3moe7q8_kindElbiiib
+    f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_bool] + [ctypes.c_int32] * 3 + [ctypes.c_bool], ctypes.c_int
+    kind = f(rows, grouped, E, K, N, gated)
+    ends = E if grouped else 0
+    if kind < 2:
+        assert -(-rows // 16) + ends <= 65535
+    elif kind < 4:
+        side = 64 if kind == 2 else 128
+        cols = -(-N * (2 if gated else 1) // side)
+        assert (-(-rows // side) + ends) * cols * 256 < 2 ** 32
+
+
 def test_binding_checks_tensors():
     torch = pytest.importorskip("torch")
     x = torch.zeros((4, 64), dtype=torch.bfloat16)
