@@ -11,11 +11,13 @@
 //    14336 x 4096 take 322 us (2.99 POP/s), 8192 x 8192 x 8192 384 (2.86; the library's product takes 542); a K step
 //    takes 1.5 us with random operands, whether they come from L2 or from memory, and 1.04 with zeros (4.1 POP/s).
 //    A tile costs some 8 us besides its K steps, which is a quarter of the time at K 2048.
-//  * tiles of 128 or 64, whose loads bound them, where whole tiles would leave compute units idle: 300 rows by 2000 x
-//    3000 8.1 us with tiles of 64, 27.5 with whole ones; 1024 by 4096 x 4096 23 with tiles of 128, 40.
+//    The last, partly filled round cuts its tiles by rows into 2, 4 or 8 for the units that would idle: 8192 rows by
+//    4608 x 14336 446 -> 390 us, 2048 by 4096 x 14336 131 -> 92.
+//  * tiles of 128 or 64, whose loads bound them, where even so whole tiles would leave compute units idle: 256 rows by
+//    3000 x 2000 7.9 us with tiles of 64, 14.4 with whole ones; 1024 by 4096 x 4096 24.4 with tiles of 128, 28.6.
 //  * 16 rows by 16 or 32 features straight from memory into registers, K divided among the waves, for a few rows of
 //    each expert: bound by the reading of the weights (32 experts of 7168 x 2048, 8 rows each: 470 MB in 83 us, 5.7
-//    TB/s) or, in small matrices, by its latency (one row by 4096 x 4096 5.9 us, 9.3 with tiles of 64).
+//    TB/s) or, in small matrices, by its latency (one row by 4096 x 4096 7.0 us, 10.9 with tiles of 64).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -59,6 +61,12 @@ __device__ __forceinline__ float silu_mul(float g, float u) {
   const float r = fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -t));
   const float e = __builtin_amdgcn_exp2f(fminf(t, 127.0f));
   return (g * u) * __builtin_amdgcn_rcpf(1.0f + fmaf(e, r * kLn2, e));
+}
+
+// The parts by rows that each of the last round's tiles is cut into, with `per` of them for the kDeal compute units
+// of an XCD: as many as there are units for, down to 32 rows.
+__host__ __device__ __forceinline__ uint32_t parts_of(uint32_t per) {
+  return per * 8 <= kDeal ? 8 : per * 4 <= kDeal ? 4 : per * 2 <= kDeal ? 2 : 1;
 }
 
 struct Item {
@@ -120,8 +128,8 @@ struct Experts {
 
 // The items of a launch.  An expert's are bands of kBandRows rows by all columns, the tiles of a band next to
 // each other; they are dealt to the XCDs (workgroups b, b + 8, ... share one) in runs of kDeal, so that the
-// compute units of an XCD read the same few weight and row tiles through its L2.  Every wave finds an item by
-// itself, 64 experts at a time, a lane each.
+// compute units of an XCD read the same few weight and row tiles through its L2 (as the parts of one tile do).
+// Every wave finds an item by itself, 64 experts at a time, a lane each.
 template <int kTile>
 struct Items {
   using X = Experts<kTile>;
@@ -142,12 +150,30 @@ struct Items {
   // Item j of XCD xcd's.  It grows with j, so that an XCD without an item j has none after it.
   __device__ __forceinline__ Item find(const Q8Args& a, uint32_t xcd, uint32_t j) const {
     const Item none{0, 0, 0, 0};
-    if (total == 0) return none;
-    const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
-    const uint32_t it = ((j / run) * kXcds + xcd) * run + j % run;
-    if (it >= total) return none;
+    if constexpr (kTile != 256) {
+      const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
+      const uint32_t it = run ? ((j / run) * kXcds + xcd) * run + j % run : 0;
+      return it < total ? at(a, it) : none;
+    } else {
+      const uint32_t whole = total / kStaying * kStaying;
+      if (j < whole / kXcds) return at(a, ((j / kDeal) * kXcds + xcd) * kDeal + j % kDeal);
+      // The last, partly filled round: its tiles are cut into as many parts by rows as there are compute units for.
+      const uint32_t per = (total - whole + kXcds - 1) / kXcds, in = j - whole / kXcds;
+      const uint32_t parts = parts_of(per);
+      const uint32_t it = whole + xcd * per + in / parts;
+      if (in >= per * parts || it >= total) return none;
+      Item found = at(a, it);
+      const int height = kTile / (int)parts, skip = (int)(in % parts) * height;
+      found.row0 += skip;
+      found.rows = min(found.rows - skip, height);
+      return found;
+    }
+  }
+
+ private:
+  __device__ __forceinline__ Item at(const Q8Args& a, uint32_t it) const {
     if (!a.offsets) return place(0, 0, (int)a.rows, total / cols, it);
-    Item found = none;
+    Item found{0, 0, 0, 0};
     if (a.experts <= 64) {
       pick(table, 0, Before{}, it, found);
       return found;
@@ -158,10 +184,9 @@ struct Items {
       if (pick(x, e0, past, it, found)) return found;
       past = x.after(a, e0);
     }
-    return none;
+    return found;
   }
 
- private:
   // Item q of an expert with rows [lo, hi) in `tiles` tiles.
   __device__ __forceinline__ Item place(int expert, int lo, int hi, uint32_t tiles, uint32_t q) const {
     constexpr uint32_t kBand = kBandRows / kTile;
@@ -774,19 +799,29 @@ hipError_t launch_tiles(const Q8Args& a, hipStream_t s) {
 Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated) {
   // What each kernel would take, in microseconds, from the rows an expert has on average (the host does not know
   // the offsets): the rounds of tiles over 256 compute units, each so many K steps of 128 bytes and something
-  // for its start and end, as measured on single matrices; and the reading of every weight, at the rate that the
-  // kernel reached where that is all.
+  // for its start and end; and the reading of every weight, at the rate in TB/s that the kernel reached where that
+  // is all.  The figures are fitted to 628 measured products (1 to 49152 rows, 1 to 128 experts, both operators):
+  // the kernel chosen takes 1.4 % longer than the best one, 31 % at most.
   const double nk = (K + kRowBytes - 1) / kRowBytes, features = (double)N * (gated ? 2 : 1);
   const double busy = grouped ? experts * (1.0 - std::pow(1.0 - 1.0 / experts, (double)rows)) : 1.0;
   const double per = rows / busy, megabytes = busy * features * K * 1e-6;
   auto tiles = [&](double x) { return grouped ? busy * (1.0 + std::max(0.0, (per - x / 2) / x)) : std::ceil(rows / x); };
   auto items = [&](double w, double x) { return tiles(x) * std::ceil(features / w) / 256.0; };
-  auto cost = [&](double work, double rate) { return std::max(work, megabytes / rate) + 0.3 * work; };
+  auto cost = [&](double work, double rate) { return std::max(work, megabytes / rate) + 0.35 * work; };
+  // A K step of a whole tile by its height: 0.41 us for 32 rows, 0.66 for 64, 0.77 for 128, 1.385 for 256.
+  auto step = [](double h) {
+    return h < 64 ? 0.41 + 0.25 * (h - 32) / 32 : h < 128 ? 0.66 + 0.11 * (h - 64) / 64 : 0.77 + 0.615 * (h - 128) / 128;
+  };
   const double whole = items(256, 256), half = items(128, 128), quarter = items(64, 64);
-  const double height = std::min(256.0, std::max(32.0, per));
-  const double step = (0.2 + 1.185 * height / 256) * std::min(1.0, 0.7 + 0.3 * whole);
+  const double height = std::min(256.0, std::max(32.0, per)), rest = whole - std::floor(whole);
+  double tall = std::floor(whole) * (nk * step(height) + 3.5);
+  if (rest > 0) {
+    const int parts = parts_of((uint32_t)std::ceil(rest * kStaying / kXcds));
+    const double idle = parts == 1 ? std::min(1.0, 0.7 + 0.3 * whole) : 1.0;  // fewer at work, at a higher clock
+    tall += nk * step(std::max(32.0, std::min(height, 256.0 / parts))) * idle + 5;
+  }
   Q8Kind best = kQ8Tiles256;
-  double least = cost(2 + std::ceil(whole) * (nk * step + 6), 4.8);
+  double least = cost(1.2 + tall, gated ? 5.5 : 4.7);
   auto consider = [&](Q8Kind kind, double c) {
     if (c < least) best = kind, least = c;
   };
@@ -794,12 +829,12 @@ Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N
   auto launches = [&](int w, int x) {
     return launch_fits(dealt(most_tiles(rows, grouped, experts, x), (int)std::ceil(features / w)), kThreads);
   };
-  if (launches(128, 128)) consider(kQ8Tiles128, cost(2 + std::ceil(half) * (nk * 0.61 + 1), 4.6));
-  if (launches(64, 64)) consider(kQ8Tiles64, cost(3 + std::max(1.0, quarter) * (nk * 0.2 + 0.3), 5.2));
+  if (launches(128, 128)) consider(kQ8Tiles128, cost(1.2 + std::ceil(half) * (nk * 0.48 + 2.8), gated ? 5.2 : 4.9));
+  if (launches(64, 64)) consider(kQ8Tiles64, cost(2.4 + std::max(1.0, quarter) * (nk * 0.21 + 0.9), gated ? 6.0 : 5.1));
   if (most_tiles(rows, grouped, experts, 16) <= kSlimTiles) {
     const double slim = items(gated ? 32 : 16, 16), slim2 = items(32, 16);
-    consider(kQ8Slim1, cost(2 + nk * std::max(0.1, (gated ? 0.14 : 0.12) * slim), 5.8));
-    if (!gated) consider(kQ8Slim2, cost(2 + nk * std::max(0.16, 0.16 * slim2), 5.8));
+    consider(kQ8Slim1, cost(2.4 + nk * std::max(0.12, 0.13 * slim), gated ? 6.1 : 6.9));
+    if (!gated) consider(kQ8Slim2, cost(2.4 + nk * 0.16 * std::max(1.0, slim2), 6.9));
   }
   return best;
 }

@@ -232,6 +232,20 @@ def test_each_kernel(counts, K, N, kind, gather, gated):
     check(run_kind(kind, x, xs, w, ws, o, index, rows, gated), reference(x, xs, w, ws, o, index, rows, gated))
 
 
+@pytest.mark.parametrize("c,N", [
+    (4100, 4096), (4353, 4352), (4600, 4600), (5000, 5000),          # 16, 50, 68 and 144 tiles in the second round
+    ([600, 0, 1500, 257, 1, 1800], 4096), ([4096], 4096)])
+def test_parts_of_the_last_round(c, N):
+    """More tiles than compute units: those of the last round are cut by rows, into as many parts as fit."""
+    rng = np.random.default_rng(17)
+    grouped = not isinstance(c, int)
+    c = c if grouped else [c]
+    off = np.concatenate([[0], np.cumsum(c)]).astype(np.int32)
+    x, xs, w, ws = make(rng, int(off[-1]), 48, N, len(c))
+    o = off if grouped else None
+    check(run_kind("tiles256", x, xs, w, ws, o, None, int(off[-1]), False), reference(x, xs, w, ws, o, None, int(off[-1]), False))
+
+
 @pytest.mark.parametrize("rows,grouped,E,K,N,gated,kind", [
     (1, False, 1, 4096, 4096, False, "slim1"), (8, False, 1, 7168, 1024, False, "slim1"),
     (96, True, 64, 1408, 2048, False, "slim2"), (96, True, 64, 2048, 1408, True, "slim1"),
