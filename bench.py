@@ -43,6 +43,7 @@ PEAK_BF16_TFLOPS = 2500.0   # MI355X dense bf16 MFMA peak
 PEAK_HBM_GBS = 8000.0
 TICK_US = 0.01              # the GPU wall clock runs at 100 MHz
 KERNEL_SRC = os.path.join(ROOT, "paper_2607_19539_amd", "csrc", "kernels.hip")
+KERNEL_HEADER = os.path.join(ROOT, "paper_2607_19539_amd", "csrc", "mma_tile.hpp")
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "producer_mixtral_traffic.md")
 
 DESCRIPTIONS = {
@@ -142,7 +143,8 @@ def cpu_baseline(wl, target_s, threads=None):
 
 def stored_traffic():
     """HBM bytes per gate/up launch from the committed counter summary, if it was taken on the
-    current kernel source (its sha256 is recorded next to the figure); else None."""
+    current kernel source (its sha256, and that of the K loops' header where they lie in one, is
+    recorded next to the figure); else None."""
     try:
         text = open(TRAFFIC_FILE).read()
     except OSError:
@@ -151,8 +153,11 @@ def stored_traffic():
     m_h = re.search(r"^kernel_sha256:\s*([0-9a-f]{64})", text, re.M)
     if not m_b or not m_h:
         return None
-    cur = hashlib.sha256(open(KERNEL_SRC, "rb").read()).hexdigest()
-    return float(m_b.group(1)) if cur == m_h.group(1) else None
+    def same(path, m):
+        return hashlib.sha256(open(path, "rb").read()).hexdigest() == m.group(1)
+
+    m_k = re.search(r"^header_sha256:\s*([0-9a-f]{64})", text, re.M)
+    return float(m_b.group(1)) if same(KERNEL_SRC, m_h) and (not m_k or same(KERNEL_HEADER, m_k)) else None
 
 
 def union_length(iv):

@@ -56,6 +56,21 @@ def test_stored_traffic_only_for_the_measured_source(bench, tmp_path, monkeypatc
 
 
 
+def test_stored_traffic_only_for_the_measured_header(bench, tmp_path, monkeypatch):
+    src, header = tmp_path / "kernels.hip", tmp_path / "mma_tile.hpp"
+    src.write_text("// kernel source\n")
+    header.write_text("// K loops\n")
+    sha = [hashlib.sha256(p.read_bytes()).hexdigest() for p in (src, header)]
+    rec = tmp_path / "traffic.md"
+    rec.write_text(f"traffic_bytes_per_launch: 3.2916e+09\nkernel_sha256: {sha[0]}\nheader_sha256: {sha[1]}\n")
+    monkeypatch.setattr(bench, "KERNEL_SRC", str(src))
+    monkeypatch.setattr(bench, "KERNEL_HEADER", str(header))
+    monkeypatch.setattr(bench, "TRAFFIC_FILE", str(rec))
+    assert bench.stored_traffic() == pytest.approx(3.2916e9)
+    header.write_text("// K loops, changed\n")
+    assert bench.stored_traffic() is None
+
+
 def test_no_share_of_peak_for_a_product_whose_sums_are_timed_elsewhere(bench):
     """Serial runs with the default split add the tail tiles' parts in the scatter launch."""
     class Wl:
