@@ -5,6 +5,7 @@
 //   w_j = scale p_j / P,  P = sum of the chosen p (or 1)
 //   gradient: dp_j = scale / P (dw_j - sum_i dw_i p_i / P) (+ dscores),
 //             softmax dl_e = p_e (dp_e - sum dp p),  sigmoid dl_e = dp_e p_e (1 - p_e)
+// 1 - p is e^-l p from l = 0 up: a difference from a p near 1 would keep none of its bits (at l = 16 6 % off).
 //
 // Many tokens are bound by vector instructions, not by memory: 32768 tokens of 256 experts take 25 us forward (1600
 // instructions for four tokens, half of them in the choice of 8; reading the logits alone would take 7) and 18 back
@@ -102,6 +103,12 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, const Place<kLan
   } else {
     load_floats<kLanes, kPer, kVec>(at, (const float*)a.logits + base, -kInf, l);
   }
+}
+
+// 1 - p of a sigmoid score p.  expf(-l) is the one that p was made with.
+__device__ __forceinline__ float sigmoid_rest(float l, float p) {
+  const float e = expf(-l);
+  return e <= 1.0f ? e * p : 1.0f - p;
 }
 
 // The token's maximum and sum, all that a softmax score needs beside its logit.
@@ -323,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   }
   if constexpr (!kSig) dot = wave_reduce<kLanes>(dot, add);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * p[i] * (1.0f - p[i]) : p[i] * (g[i] - dot);
+  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * p[i] * sigmoid_rest(l[i], p[i]) : p[i] * (g[i] - dot);
   const int64_t base = at.t * a.experts + at.e0;
 #pragma unroll
   for (int i = 0; i < kPer; i += kVec ? 4 : 1) {
