@@ -3,8 +3,10 @@
 //
 //   p = softmax(l) or sigmoid(l);  pick = p + bias;  ids = top k of pick within the best groups
 //   w_j = scale p_j / P,  P = sum of the chosen p (or 1)
-//   gradient: dp_j = scale / P (dw_j - sum_i dw_i p_i / P) (+ dscores),
-//             softmax dl_e = p_e (dp_e - sum dp p),  sigmoid dl_e = dp_e p_e (1 - p_e)
+//   gradient: u_j = scale p_j / P (dw_j - sum_i dw_i p_i / P),  u_e += p_e dscores_e,
+//             softmax dl_e = u_e - p_e sum u,  sigmoid dl_e = u_e (1 - p_e)
+// u is the scores' gradient times the scores.  The gradient itself would overflow where the chosen scores sum to less
+// than scale / 2^128, as a bias can make them; p_j / P is at most 1.
 // 1 - p is e^-l p from l = 0 up: a difference from a p near 1 would keep none of its bits (at l = 16 6 % off).
 //
 // Many tokens are bound by vector instructions, not by memory: 32768 tokens of 256 experts take 25 us forward (1600
@@ -302,35 +304,35 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) g[i] = 0.0f;
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) grads[at.lane * kPer + i] = g[i];
   const Softmax sm = softmax_of<kSig, kLanes, kPer>(at, l);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) p[i] = score<kSig>(l[i], sm);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) grads[at.lane * kPer + i] = a.dscores ? p[i] * g[i] : 0.0f;
   const float v = have ? score<kSig>(own, sm) : 0.0f;
-  float dp = dw * a.scale;
+  float u = a.scale * v * dw;
   if (a.renormalise) {
-    const float total = wave_reduce<kLanes>(v, add);
-    const float mean = wave_reduce<kLanes>(dw * v, add) / total;
-    dp = total > 0.0f || total != total ? a.scale / total * (dw - mean) : 0.0f;
+    const float total = wave_reduce<kLanes>(v, add), share = v / total;
+    const float mean = wave_reduce<kLanes>(dw * share, add);
+    u = total > 0.0f || total != total ? a.scale * share * (dw - mean) : 0.0f;
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   // One choice at a time, as ids may repeat: a wave's LDS operations happen in their order.
   const int slot = have ? id / at.run * kPer + id % at.run : 0;
   for (int j = 0; j < a.k; ++j)
-    if (at.lane == j && have) atomicAdd(&grads[slot], dp);
+    if (at.lane == j && have) atomicAdd(&grads[slot], u);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   float dot = 0.0f;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     g[i] = grads[at.lane * kPer + i];
-    dot += g[i] * p[i];
+    dot += g[i];
   }
   if constexpr (!kSig) dot = wave_reduce<kLanes>(dot, add);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * p[i] * sigmoid_rest(l[i], p[i]) : p[i] * (g[i] - dot);
+  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * sigmoid_rest(l[i], p[i]) : g[i] - p[i] * dot;
   const int64_t base = at.t * a.experts + at.e0;
 #pragma unroll
   for (int i = 0; i < kPer; i += kVec ? 4 : 1) {

@@ -80,3 +80,32 @@ def test_sigmoid_scores_at_the_ends():
     for j in range(0, 8, 2):
         got = run_backward(cfg, l, np.array([[j, j + 1]], np.int32), np.ones((1, 2), np.float32), np.ones((1, 8), np.float32))
         assert np.all(np.abs(got) < 1e-37)
+
+
+@pytest.mark.parametrize("dscores", [False, True])
+@pytest.mark.parametrize("T", [29, 2061])
+@pytest.mark.parametrize("scale", [2.5, 50.0])
+@pytest.mark.parametrize("k", [1, 3])
+@pytest.mark.parametrize("score", [SOFT, SIG])
+def test_chosen_scores_that_sum_to_a_subnormal(score, k, scale, T, dscores):
+    """A bias can steer a token to experts whose scores are below 2^-126; scale over their sum overflows (three
+    sigmoid scores by 2.5 aside), the shares do not."""
+    cfg = B.make_route_config(16, k, score=score, scale=scale)
+    log(f"route backward, tiny scores {score} k={k} T={T} dscores={dscores}")
+    rng = np.random.default_rng(T + k)
+    ids = choices(rng, T, 16, k)
+    if score == SOFT:
+        # One expert, not a chosen one, has nearly all of the sum; the chosen have e^-92 to e^-90 of it.
+        l = rng.uniform(-4, -2, (T, 16))
+        np.put_along_axis(l, ids.astype(np.int64), rng.uniform(-92, -90, (T, k)), 1)
+        for t in range(T):
+            l[t, np.setdiff1d(np.arange(16), ids[t])[0]] = 0.0
+    else:
+        l = rng.uniform(-3, 3, (T, 16))
+        np.put_along_axis(l, ids.astype(np.int64), rng.uniform(-88.5, -87.5, (T, k)), 1)
+    l = l.astype(np.float32)
+    p = np.take_along_axis(score64(l, score), ids.astype(np.int64), 1).sum(1)
+    assert np.all((p > 1e-41) & (p < 4e-38)) and ((p < scale / 3.4e38).any() or (score, k, scale) == (SIG, 3, 2.5))
+    dw = rng.standard_normal((T, k)).astype(np.float32)
+    ds = rng.standard_normal((T, 16)).astype(np.float32) if dscores else None
+    check(cfg, l, ids, dw, ds)
