@@ -51,16 +51,20 @@ struct Shape {
   static __device__ __forceinline__ bool up(int n) { return gated && (n / (kW / 4)) & 1; }
 };
 
-// silu(g) * u = g u / (1 + e^-g) with the hardware's exponential and reciprocal, each within one fp32 ulp.  The
-// exponent -g log2(e) is rounded, which would cost e^-g an error of |g| 2^-24; the rounding is made good in the
-// first order (e (1 + r ln 2), four instructions), as a bf16 result that falls the other way may change the row's
-// 8-bit scale after it.  A large negative g gives e^-g = inf, a reciprocal of 0 and a result of 0.
-__device__ __forceinline__ float silu_mul(float g, float u) {
-  constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147181f;
-  const float t = -g * kLog2e;
-  const float r = fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -t));
-  const float e = __builtin_amdgcn_exp2f(fminf(t, 127.0f));
-  return (g * u) * __builtin_amdgcn_rcpf(1.0f + fmaf(e, r * kLn2, e));
+// silu(g) * u = (g / (1 + e^-g)) u, from a quarter of g, with the hardware's exponential and reciprocal, each within
+// one fp32 ulp.  The exponent t = -g log2(e) is rounded, which would cost e^-g an error of |g| 2^-24; the rounding r is
+// made good in the first order (e^-g (1 + r ln 2)), as a bf16 result that falls the other way may change the row's
+// 8-bit scale after it.  With a quarter of 1 + e^-g, too, the reciprocal is never a subnormal, which the hardware
+// would flush: it is 2^-126 or more, and 0 from t = 128 on, where e^-g is infinite in fp32.  Where t itself overflows
+// r is infinite; its factor is kept near a quarter.  u comes last, as g u may overflow where silu(g) u does not.
+constexpr float kGateShare = 0.25f;
+__device__ __forceinline__ float silu_mul(float quarter_g, float u) {
+  constexpr float kLog2e = 4 * 1.44269504f, kLog2eRest = 4 * 1.92596303e-8f, kLn2 = 0.693147181f;
+  constexpr float kLow = 0.15915494f, kHigh = 0.5f;  // constants that an instruction holds
+  const float t = -quarter_g * kLog2e;
+  const float r = fmaf(-quarter_g, kLog2eRest, fmaf(-quarter_g, kLog2e, -t));
+  const float factor = __builtin_amdgcn_fmed3f(fmaf(r, kLn2 / 4, 0.25f), kLow, kHigh);
+  return quarter_g * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), factor, 0.25f)) * u;
 }
 
 // The parts by rows that each of the last round's tiles is cut into, with `per` of them for the kDeal compute units
@@ -372,9 +376,8 @@ __device__ __forceinline__ void small_item(const Q8Args& a, const Item& it, uint
 #pragma unroll
   for (int i = 0; i < (gated ? kNI / 2 : kNI); ++i) {
     const int n = quad_n(i);
-    const f32x4 ws = *(const f32x4*)(scales + n);
-    f32x4 ws3 = {};
-    if constexpr (gated) ws3 = *(const f32x4*)(scales + n + kW / 4);
+    f32x4 ws = *(const f32x4*)(scales + n), ws3 = {};
+    if constexpr (gated) ws *= kGateShare, ws3 = *(const f32x4*)(scales + n + kW / 4);
 #pragma unroll
     for (int j = 0; j < kNJ; ++j) {
       float v[4];
@@ -553,7 +556,10 @@ __device__ __forceinline__ void tile_item(const Q8Args& a, const Item& it, const
 #pragma unroll
   for (int i = 0; i < kQuads; ++i) {
     asm volatile("" ::"v"(ws[i]));
-    if constexpr (gated) asm volatile("" ::"v"(ws3[i]));
+    if constexpr (gated) {
+      asm volatile("" ::"v"(ws3[i]));
+      ws[i] *= kGateShare;
+    }
   }
   if (next.rows > 0) {
     src.addresses(a, next);
@@ -756,7 +762,7 @@ __global__ __launch_bounds__(kThreads) void q8_slim_kernel(Q8Args a) {
       const float* ws = (q ? a.ws3 : a.ws) + wofs + n;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float p = (float)s[t] * (xs * ws[t]);
+        const float p = (float)s[t] * (xs * (gated && !q ? ws[t] * kGateShare : ws[t]));
         v[t] = q ? silu_mul(v[t], p) : p;
       }
     }
