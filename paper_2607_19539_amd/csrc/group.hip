@@ -14,6 +14,7 @@
 
 #include <algorithm>
 
+#include "launch.hpp"
 #include "ops.hpp"
 #include "vec_device.hpp"
 
@@ -185,14 +186,11 @@ hipError_t launch_group(const GroupArgs& a, hipStream_t s) {
   const uint32_t lds = (uint32_t)(std::max(kWaves * a.experts, 2 * kThreads) * sizeof(int));
   if (blocks == 0) {
     const int64_t entries = ((int64_t)a.n + kThreads - 1) / kThreads * kThreads;
-    hipLaunchKernelGGL(group_place_kernel<true>, dim3(1), dim3(kThreads), lds, s, a, entries, bits);
-    return hipGetLastError();
+    return launch(group_place_kernel<true>, dim3(1), dim3(kThreads), lds, s, a, entries, bits);
   }
   const int64_t entries = block_entries(a.n);
-  hipLaunchKernelGGL(group_count_kernel, dim3(blocks), dim3(kThreads), lds, s, a, entries);
-  if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL(group_place_kernel<false>, dim3(blocks), dim3(kThreads), lds, s, a, entries, bits);
-  return hipGetLastError();
+  if (hipError_t e = launch(group_count_kernel, dim3(blocks), dim3(kThreads), lds, s, a, entries)) return e;
+  return launch(group_place_kernel<false>, dim3(blocks), dim3(kThreads), lds, s, a, entries, bits);
 }
 
 }  // namespace moe

@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "launch.hpp"
 #include "ops.hpp"
 #include "vec_device.hpp"
 
@@ -202,18 +203,14 @@ void by_row(int64_t rows, int32_t H, F&& f) {
 }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
-  bool fits = true;
+  hipError_t e = hipErrorInvalidConfiguration;
   by_row(a.rows, a.H, [&](auto lanes, auto vecs) {
     constexpr int L = decltype(lanes)::value, V = decltype(vecs)::value, kRows = row_threads(L) / L;
     const int64_t blocks = (a.rows + kRows - 1) / kRows;
-    const dim3 grid((uint32_t)blocks);
-    if (!(fits = launch_fits(blocks, row_threads(L)))) return;
-    if (a.weight)
-      hipLaunchKernelGGL((norm_kernel<L, V, true>), grid, dim3(row_threads(L)), 0, s, a);
-    else
-      hipLaunchKernelGGL((norm_kernel<L, V, false>), grid, dim3(row_threads(L)), 0, s, a);
+    if (!launch_fits(blocks, row_threads(L))) return;
+    e = launch(a.weight ? norm_kernel<L, V, true> : norm_kernel<L, V, false>, dim3((uint32_t)blocks), dim3(row_threads(L)), 0, s, a);
   });
-  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
+  return e;
 }
 
 // ------------------------------------------------------------------------------------ gradients
@@ -391,30 +388,25 @@ hipError_t launch_norm_backward(const NormBackwardArgs& args, hipStream_t s) {
   NormBackwardArgs a = args;
   const int64_t parts = a.rows > 0 ? norm_backward_parts(a.rows, a.H) : 0;
   if (parts == 1) a.parts = a.dweight;
-  const dim3 grid((uint32_t)parts), threads(kBackThreads);
   const int nvec = a.H / 8;
-  if (parts == 0) {
-    // no rows: dweight becomes zeros below
-  } else if (a.H > kWideRow) {
-    hipLaunchKernelGGL(norm_backward_wide_kernel, grid, threads, 0, s, a);
-  } else if (nvec <= 64) {
-    hipLaunchKernelGGL((norm_backward_kernel<64, 1>), grid, threads, 0, s, a);
-  } else if (nvec <= 128) {
-    hipLaunchKernelGGL((norm_backward_kernel<64, 2>), grid, threads, 0, s, a);
-  } else if (back_lanes(a.H) == 64) {
-    hipLaunchKernelGGL((norm_backward_kernel<64, 4>), grid, threads, 0, s, a);
-  } else if (back_lanes(a.H) == 128) {
-    hipLaunchKernelGGL((norm_backward_kernel<128, 4>), grid, threads, 0, s, a);
-  } else if (back_lanes(a.H) == 256) {
-    hipLaunchKernelGGL((norm_backward_kernel<256, 4>), grid, threads, 0, s, a);
-  } else {
-    hipLaunchKernelGGL((norm_backward_kernel<kBackThreads, 4>), grid, threads, 0, s, a);
-  }
-  if (hipError_t e = hipGetLastError()) return e;
+  auto kernel = norm_backward_kernel<kBackThreads, 4>;
+  if (a.H > kWideRow)
+    kernel = norm_backward_wide_kernel;
+  else if (nvec <= 64)
+    kernel = norm_backward_kernel<64, 1>;
+  else if (nvec <= 128)
+    kernel = norm_backward_kernel<64, 2>;
+  else if (back_lanes(a.H) == 64)
+    kernel = norm_backward_kernel<64, 4>;
+  else if (back_lanes(a.H) == 128)
+    kernel = norm_backward_kernel<128, 4>;
+  else if (back_lanes(a.H) == 256)
+    kernel = norm_backward_kernel<256, 4>;
+  if (parts > 0)  // no rows: dweight becomes zeros below
+    if (hipError_t e = launch(kernel, dim3((uint32_t)parts), dim3(kBackThreads), 0, s, a)) return e;
   if (parts == 1) return hipSuccess;
-  hipLaunchKernelGGL(norm_weight_kernel, dim3((a.H + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumRows), 0, s, a.parts,
-                     (int)parts, a.H, a.dweight);
-  return hipGetLastError();
+  return launch(norm_weight_kernel, dim3((a.H + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumRows), 0, s, a.parts,
+                (int)parts, a.H, a.dweight);
 }
 
 // ------------------------------------------------------------------------------------ back to bf16
@@ -439,11 +431,7 @@ hipError_t launch_restore(const RestoreArgs& a, hipStream_t s) {
   const bool wave = a.H <= 2048;
   const int64_t blocks = wave ? (a.rows + 3) / 4 : a.rows;
   if (!launch_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  if (wave)
-    hipLaunchKernelGGL(restore_kernel<64>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(restore_kernel<256>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch(wave ? restore_kernel<64> : restore_kernel<256>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
 }
 
 }  // namespace moe

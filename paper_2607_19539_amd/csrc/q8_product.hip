@@ -24,6 +24,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "launch.hpp"
 #include "mma_tile.hpp"
 #include "ops.hpp"
 #include "vec_device.hpp"
@@ -785,8 +786,7 @@ template <bool gated, int kN>
 hipError_t launch_slim(const Q8Args& a, hipStream_t s) {
   const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, 16);
   if (tiles > kSlimTiles) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((q8_slim_kernel<gated, kN, 1>), dim3((a.N + 16 * kN - 1) / (16 * kN), (uint32_t)tiles), dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  return launch(q8_slim_kernel<gated, kN, 1>, dim3((a.N + 16 * kN - 1) / (16 * kN), (uint32_t)tiles), dim3(kThreads), 0, s, a);
 }
 
 template <bool gated, int kW, int kX>
@@ -796,10 +796,9 @@ hipError_t launch_tiles(const Q8Args& a, hipStream_t s) {
   const int64_t grid = dealt(tiles, cols);
   if (kW == 256 ? grid > INT32_MAX : !launch_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   if constexpr (kW == 256)
-    hipLaunchKernelGGL(q8_tile_kernel<gated>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
+    return launch(q8_tile_kernel<gated>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
   else
-    hipLaunchKernelGGL((q8_small_kernel<gated, kW, kX>), dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
-  return hipGetLastError();
+    return launch(q8_small_kernel<gated, kW, kX>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
 }
 
 Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated) {

@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "launch.hpp"
 #include "ops.hpp"
 #include "vec_device.hpp"
 
@@ -403,25 +404,25 @@ int64_t token_blocks(const RouteArgs& a, int lanes) {
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s) {
-  bool fits = true;
+  hipError_t e = hipErrorInvalidConfiguration;
   by_shape(a, nullptr, a.bias, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
     const int64_t blocks = token_blocks(a, L);
-    if (!(fits = launch_fits(blocks, kThreads))) return;
-    hipLaunchKernelGGL((route_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
+    if (!launch_fits(blocks, kThreads)) return;
+    e = launch(route_kernel<L, P, decltype(vec)::value, decltype(sig)::value>, dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
   });
-  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
+  return e;
 }
 
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s) {
-  bool fits = true;
+  hipError_t e = hipErrorInvalidConfiguration;
   by_shape(a, a.dlogits, a.dscores, [&](auto lanes, auto per, auto vec, auto sig) {
     constexpr int L = decltype(lanes)::value, P = decltype(per)::value;
     const int64_t blocks = token_blocks(a, L);
-    if (!(fits = launch_fits(blocks, kThreads))) return;
-    hipLaunchKernelGGL((route_backward_kernel<L, P, decltype(vec)::value, decltype(sig)::value>), dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
+    if (!launch_fits(blocks, kThreads)) return;
+    e = launch(route_backward_kernel<L, P, decltype(vec)::value, decltype(sig)::value>, dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
   });
-  return fits ? hipGetLastError() : hipErrorInvalidConfiguration;
+  return e;
 }
 
 }  // namespace moe
