@@ -17,6 +17,7 @@
 
 #include "combine_split.hpp"
 #include "kernels.hpp"
+#include "launch.hpp"
 
 namespace moe {
 
@@ -111,16 +112,15 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(CombineArgs a)
 }
 
 template <int kVec>
-hipError_t launch(const CombineArgs& a, hipStream_t s) {
+hipError_t launch_vec(const CombineArgs& a, hipStream_t s) {
   const dim3 grid((uint32_t)combine_spans(a.H, kVec), (uint32_t)std::min<int64_t>(a.tokens, 65535));
-  hipLaunchKernelGGL((combine_kernel<kVec>), grid, dim3(kCombineThreads), 0, s, a);
-  return hipGetLastError();
+  return launch(combine_kernel<kVec>, grid, dim3(kCombineThreads), 0, s, a);
 }
 
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
   if (a.tokens <= 0) return hipSuccess;
   const int vec = combine_vec(a.tokens, a.k, a.H);
-  return vec == 1 ? launch<1>(a, s) : vec == 2 ? launch<2>(a, s) : launch<4>(a, s);
+  return vec == 1 ? launch_vec<1>(a, s) : vec == 2 ? launch_vec<2>(a, s) : launch_vec<4>(a, s);
 }
 
 }  // namespace moe

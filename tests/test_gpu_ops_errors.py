@@ -36,13 +36,13 @@ def calls():
     return out
 
 
-def test_an_error_left_behind_is_not_the_operators():
+def run_after_an_error(todo):
+    """The calls that report an error which an earlier call left behind, and whether each leaves it."""
     lib = B.load()
     hip = {n: getattr(lib, n) for n in ("hipSetDevice", "hipPeekAtLastError", "hipGetLastError")}  # of the runtime it is linked to
     for f in hip.values():
         f.restype = ctypes.c_int
     hip["hipSetDevice"].argtypes = [ctypes.c_int]
-    todo = calls()
     for call in todo.values():
         call()
     torch.cuda.synchronize()
@@ -58,4 +58,16 @@ def test_an_error_left_behind_is_not_the_operators():
         kept.append(hip["hipPeekAtLastError"]() == left)
         hip["hipGetLastError"]()
     torch.cuda.synchronize()
+    return reported, kept
+
+
+def test_an_error_left_behind_is_not_the_operators():
+    reported, kept = run_after_an_error(calls())
     assert not reported and all(kept)
+
+
+def test_an_error_left_behind_is_not_the_combines():
+    recv, gate = torch.ones((12, 64), dtype=torch.bfloat16, device="cuda"), torch.ones((4, 2), device="cuda")
+    slot, out = torch.zeros((4, 2), dtype=torch.int32, device="cuda"), torch.empty((4, 64), dtype=torch.bfloat16, device="cuda")
+    reported, kept = run_after_an_error(dict(combine=lambda: B.moe_combine(recv, slot, gate, out)))
+    assert not reported and all(kept) and bool((out == 2).all())
