@@ -535,7 +535,7 @@ int moe_group(const int32_t* ids, int64_t tokens, int32_t k, int32_t experts, in
  * its.  row_index holds `rows` entries (moe_group's row_token); an entry outside [0, x_rows) makes its
  * row of out NaN.  Without row_index x_rows has to be at least rows.
  * in_features: a multiple of 16, at most 131056 (no 32-bit sum overflows); out_features: a multiple
- * of 8; experts: at most 1024; with row_index x_rows * in_features below 2^32.
+ * of 8, at most 2^31 - 512; experts: at most 1024; with row_index x_rows * in_features below 2^32.
  */
 int moe_q8_product(const void* xq, const float* x_scale, int64_t x_rows, const int32_t* row_index,
                    const int32_t* expert_offsets, int32_t experts, const void* w, const float* w_scale, int64_t rows,

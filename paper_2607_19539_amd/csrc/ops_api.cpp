@@ -16,10 +16,12 @@ constexpr int32_t kMaxChoices = 64;
 constexpr int32_t kMaxGroups = 64;
 constexpr int32_t kMaxInFeatures = 131056;  // 2^17 - 16: |sum| of products of up to 128 * 127 stays below 2^31
 
+constexpr int32_t kMaxOutFeatures = INT32_MAX - 511;  // kernels number the features of a last tile that is not full, too
+
 bool misaligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) != 0; }
 
 int launched(hipError_t e, const char* who) {
-  if (e == hipErrorInvalidConfiguration) return record_error(MOE_EUNSUPPORTED, who, "more rows than one launch takes");
+  if (e == hipErrorInvalidConfiguration) return record_error(MOE_EUNSUPPORTED, who, "more rows or features than one launch takes");
   return e == hipSuccess ? MOE_OK : record_error(MOE_EHIP, who, hipGetErrorString(e));
 }
 
@@ -74,7 +76,8 @@ int q8(const char* who, bool gated, const Q8Args& a, void* stream) {
   if (!a.index && a.x_rows < a.rows) return record_error(MOE_EINVAL, who, "fewer rows of xq than of out");
   if (a.K % 16 || a.K > kMaxInFeatures)
     return record_error(MOE_EUNSUPPORTED, who, "in_features must be a multiple of 16, <= 131056");
-  if (a.N % 8) return record_error(MOE_EUNSUPPORTED, who, "out_features must be a multiple of 8");
+  if (a.N % 8 || a.N > kMaxOutFeatures)
+    return record_error(MOE_EUNSUPPORTED, who, "out_features must be a multiple of 8, <= 2^31 - 512");
   if (a.experts > kMaxExperts) return record_error(MOE_EUNSUPPORTED, who, "at most 1024 experts");
   if (a.rows > INT32_MAX || a.x_rows > INT32_MAX) return record_error(MOE_EUNSUPPORTED, who, "rows must be below 2^31");
   if (a.index && (uint64_t)a.x_rows * (uint64_t)a.K > UINT32_MAX)

@@ -778,6 +778,9 @@ int64_t most_tiles(int64_t rows, bool grouped, int32_t experts, int height) {
 
 constexpr int64_t kSlimTiles = 65535;  // they are the grid's second axis
 
+// Workgroups along the features of a slim kernel of 16 `n` features (gated: of each matrix).
+int64_t slim_cols(int32_t N, int n) { return ((int64_t)N + 16 * n - 1) / (16 * n); }
+
 int64_t dealt(int64_t tiles, int cols) {
   return (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
 }
@@ -785,8 +788,9 @@ int64_t dealt(int64_t tiles, int cols) {
 template <bool gated, int kN>
 hipError_t launch_slim(const Q8Args& a, hipStream_t s) {
   const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, 16);
-  if (tiles > kSlimTiles) return hipErrorInvalidConfiguration;
-  return launch(q8_slim_kernel<gated, kN, 1>, dim3((a.N + 16 * kN - 1) / (16 * kN), (uint32_t)tiles), dim3(kThreads), 0, s, a);
+  const int64_t cols = slim_cols(a.N, kN);
+  if (tiles > kSlimTiles || !launch_fits(cols, kThreads)) return hipErrorInvalidConfiguration;
+  return launch(q8_slim_kernel<gated, kN, 1>, dim3((uint32_t)cols, (uint32_t)tiles), dim3(kThreads), 0, s, a);
 }
 
 template <bool gated, int kW, int kX>
@@ -838,8 +842,8 @@ Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N
   if (launches(64, 64)) consider(kQ8Tiles64, cost(2.4 + std::max(1.0, quarter) * (nk * 0.21 + 0.9), gated ? 6.0 : 5.1));
   if (most_tiles(rows, grouped, experts, 16) <= kSlimTiles) {
     const double slim = items(gated ? 32 : 16, 16), slim2 = items(32, 16);
-    consider(kQ8Slim1, cost(2.4 + nk * std::max(0.12, 0.13 * slim), gated ? 6.1 : 6.9));
-    if (!gated) consider(kQ8Slim2, cost(2.4 + nk * 0.16 * std::max(1.0, slim2), 6.9));
+    if (launch_fits(slim_cols(N, 1), kThreads)) consider(kQ8Slim1, cost(2.4 + nk * std::max(0.12, 0.13 * slim), gated ? 6.1 : 6.9));
+    if (!gated && launch_fits(slim_cols(N, 2), kThreads)) consider(kQ8Slim2, cost(2.4 + nk * 0.16 * std::max(1.0, slim2), 6.9));
   }
   return best;
 }

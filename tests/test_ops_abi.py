@@ -200,3 +200,30 @@ def test_binding_checks_tensors():
         B.moe_q8_product(q, w, torch.zeros((2, 8, 64), dtype=torch.int8), w, torch.zeros((4, 8), dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="at least"):
         B.moe_q8_product(q, w, torch.zeros((1, 8, 64), dtype=torch.int8), w, torch.zeros((5, 8), dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,grouped,E,K,N", [
+    (1, False, 1, 16, 2 ** 28 - 8), (1, False, 1, 16, 2 ** 28), (1, False, 1, 16, 2 ** 29), (1, False, 1, 128, 2 ** 30),
+    (8, True, 4, 16, 2 ** 28), (1, False, 1, 16, 2 ** 31 - 512)])
+def test_the_product_chosen_for_many_features_can_be_launched(rows, grouped, E, K, N, gated):
+    """A workgroup for 16 or 32 features each, or for a tile's: a launch has fewer than 2^32 threads."""
+    f = B.load()._ZN3moe7q8_kindElbiiib
+    f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_bool] + [ctypes.c_int32] * 3 + [ctypes.c_bool], ctypes.c_int
+    kind, ends = f(rows, grouped, E, K, N, gated), E if grouped else 0
+    if kind < 2:
+        assert -(-N // (32 if kind == 1 and not gated else 16)) * 256 < 2 ** 32
+    elif kind < 4:
+        side = 64 if kind == 2 else 128
+        assert (-(-rows // side) + ends) * -(-N * (2 if gated else 1) // side) * 256 < 2 ** 32
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("N", [2 ** 31 - 504, 2 ** 31 - 256, 2 ** 31 - 8])
+def test_features_past_the_last_tile_have_a_32_bit_number(N, gated):
+    lib = B.load()
+    if gated:
+        rc = lib.moe_q8_gated(P, P, 4, None, None, 1, P, P, P, P, 4, 64, N, P, None)
+    else:
+        rc = lib.moe_q8_product(P, P, 4, None, None, 1, P, P, 4, 64, N, P, None)
+    assert rc == B.MOE_EUNSUPPORTED and "out_features" in B.moe_stage_last_error(None)
