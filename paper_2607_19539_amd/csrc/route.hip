@@ -7,7 +7,7 @@
 //             softmax dl_e = u_e - p_e sum u,  sigmoid dl_e = u_e (1 - p_e)
 // u is the scores' gradient times the scores.  The gradient itself would overflow where the chosen scores sum to less
 // than scale / 2^128, as a bias can make them; p_j / P is at most 1.
-// 1 - p is e^-l p from l = 0 up: a difference from a p near 1 would keep none of its bits (at l = 16 6 % off).
+// 1 - p is taken as e^-l p: a difference from a p near 1 would keep few of its bits (at l = 16 it is 6 % off).
 //
 // Many tokens are bound by vector instructions, not by memory: 32768 tokens of 256 experts take 25 us forward (1600
 // instructions for four tokens, half of them in the choice of 8; reading the logits alone would take 7) and 18 back
@@ -108,11 +108,8 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, const Place<kLan
   }
 }
 
-// 1 - p of a sigmoid score p.  expf(-l) is the one that p was made with.
-__device__ __forceinline__ float sigmoid_rest(float l, float p) {
-  const float e = expf(-l);
-  return e <= 1.0f ? e * p : 1.0f - p;
-}
+// 1 - p of a sigmoid score p, from the exponential that p was made with; where that is infinite, p is 0.
+__device__ __forceinline__ float sigmoid_rest(float l, float p) { return fminf(expf(-l), 0x1.fffffep127f) * p; }
 
 // The token's maximum and sum, all that a softmax score needs beside its logit.
 struct Softmax {
@@ -307,9 +304,11 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   }
   const Softmax sm = softmax_of<kSig, kLanes, kPer>(at, l);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) p[i] = score<kSig>(l[i], sm);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) grads[at.lane * kPer + i] = a.dscores ? p[i] * g[i] : 0.0f;
+  for (int i = 0; i < kPer; ++i) {
+    p[i] = score<kSig>(l[i], sm);
+    grads[at.lane * kPer + i] = p[i] * g[i];
+    if constexpr (kSig) p[i] = sigmoid_rest(l[i], p[i]);  // all that is asked of it from here on
+  }
   const float v = have ? score<kSig>(own, sm) : 0.0f;
   float u = a.scale * v * dw;
   if (a.renormalise) {
@@ -333,7 +332,7 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteArgs a) {
   }
   if constexpr (!kSig) dot = wave_reduce<kLanes>(dot, add);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * sigmoid_rest(l[i], p[i]) : g[i] - p[i] * dot;
+  for (int i = 0; i < kPer; ++i) g[i] = kSig ? g[i] * p[i] : g[i] - p[i] * dot;
   const int64_t base = at.t * a.experts + at.e0;
 #pragma unroll
   for (int i = 0; i < kPer; i += kVec ? 4 : 1) {
