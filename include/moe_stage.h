@@ -492,7 +492,7 @@ typedef struct {
  *   weights = scale * p[ids] (/ sum of p[ids], with renormalise)
  * ids [tokens, k] int32, weights [tokens, k] fp32, scores (optional) p [tokens, experts] fp32.
  * Equal picks go to the lower index, for experts and for groups.  An expert whose logit or pick is
- * -infinity is never chosen (its p is 0); where fewer than k are left, the rest of a token's ids are -1
+ * -infinity is never chosen (with a logit of -infinity its p is 0 too); where fewer than k are left, the rest of a token's ids are -1
  * and their weights 0.  Where the chosen scores sum to 0 the weights are 0.  A token with a NaN among
  * its picks (a NaN logit or bias, or +infinity under a softmax) gets the ids 0 .. k-1 with NaN weights,
  * so that the error shows in what is computed from it.

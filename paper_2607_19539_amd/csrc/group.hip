@@ -6,9 +6,10 @@
 // which wave runs first.  Up to kOneEntries one workgroup does it all in one launch; more are counted by a
 // first launch, from whose counts each workgroup of the second finds where its entries of each expert begin.
 //
-// Nothing here is much data (12 bytes an entry): what counts is the chain of dependent steps and, for many entries,
-// the scattered stores of row_token.  384 entries of 256 experts take 3.5 us in one launch, 262144 take 2.7 + 9.6
-// (a third launch that summed the counts by itself took 81).
+// Nothing here is much data (12 bytes an entry): what counts is the chain of dependent steps.  384 entries of 256
+// experts take 3.6 us in one launch, 262144 take 3.0 + 9.6 (a third launch that summed the counts by itself took 81).
+// Of the 9.6 some 4.4 are vector instructions, 660 for each of four waves a SIMD on half of the compute units: the
+// reading of every workgroup's counts, the counting of the own entries once more, the ranks.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

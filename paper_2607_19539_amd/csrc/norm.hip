@@ -8,7 +8,7 @@
 // Each row is read once, held in registers as its packed bf16, and each output is written once; memory bounds
 // them all: 4096 rows of 7168 with the sum and 8 bits out 40 us (205 MB, 5.2 TB/s), 8192 rows of 14336 to 8 bits
 // 55 us (352 MB, 6.4 TB/s), back to bf16 4096 of 7168 14 us (88 MB, 6.3 TB/s), the gradients of 8192 rows of 2048
-// 24 + 3 us (135 MB).  Read three times over from memory, as a first version did, the first took 88 us.  A few rows
+// 24 + 5 us (135 MB).  Read three times over from memory, as a first version did, the first took 88 us.  A few rows
 // are bound by their chain (loads, one or two reductions, stores): 16 of 4096 take 3.4 us.
 // Sums are fp32; h is rounded to bf16 before it is normed, so that the gradients, which start from the stored h,
 // are those of the very function that was computed.

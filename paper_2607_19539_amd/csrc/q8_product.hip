@@ -7,9 +7,11 @@
 //
 // Three kinds of kernel, chosen by an estimate of each one's time (q8_kind):
 //  * whole tiles of 256 weight rows by up to 256 rows on the K loops of mma_tile.hpp, one workgroup a compute unit
-//    that stays and starts its next tile's loads under the epilogue.  The chip's power bounds them: 8192 rows by
-//    14336 x 4096 take 322 us (2.99 POP/s), 8192 x 8192 x 8192 384 (2.86; the library's product takes 542); a K step
-//    takes 1.5 us with random operands, whether they come from L2 or from memory, and 1.04 with zeros (4.1 POP/s).
+//    that stays and starts its next tile's loads under the epilogue.  Their K steps bound them: 8192 rows by
+//    14336 x 4096 take 322 us (2.99 POP/s), 8192 x 8192 x 8192 384 (2.86; the library's product takes 542).  A step
+//    takes 1.5 us with random operands, whether they come from L2 or from memory, which at the clock it then runs at
+//    (1.96 GHz) is 2900 cycles for 2048 of matrix instructions, and 1.04 us with zeros (4.1 POP/s): power counts, but
+//    what the other third of the cycles waits for has not been taken apart.
 //    A tile costs some 8 us besides its K steps, which is a quarter of the time at K 2048.
 //    The last, partly filled round cuts its tiles by rows into 2, 4 or 8 for the units that would idle: 8192 rows by
 //    4608 x 14336 446 -> 390 us, 2048 by 4096 x 14336 131 -> 92.

@@ -10,8 +10,8 @@
 // 1 - p is taken as e^-l p: a difference from a p near 1 would keep few of its bits (at l = 16 it is 6 % off).
 //
 // Many tokens are bound by vector instructions, not by memory: 32768 tokens of 256 experts take 25 us forward (1600
-// instructions for four tokens, half of them in the choice of 8; reading the logits alone would take 7) and 18 back
-// (67 MB, 3.7 TB/s).  A few are bound by the chain of the choices: 32 of 256 take 5 us.
+// instructions for four tokens, half of them in the choice of 8; reading the logits alone would take 7) and 18 to 19
+// back (71 MB, 3.8 TB/s).  A few are bound by the chain of the choices: 32 of 256 take 5 us.
 //
 // kLanes lanes take a token; lane i holds the experts i * run .. i * run + run - 1 (run <= kPer) in registers.
 // A score has to come out the same however it is computed, or near ties fall differently from one pass (or one
@@ -356,7 +356,7 @@ template <class F>
 void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
   // Few lanes to a token cost the least work in all (a reduction over 16 is four steps, and four tokens share
   // each): 32768 tokens of 256 experts 25 us with 16 lanes, 69 with 64; 21082 of 384 and back 34 with 32 lanes, 43
-  // with 64.  64 lanes have the shorter chain, for few tokens.
+  // with 64.  64 lanes have the shorter chain, for few tokens.  A choice has a lane, so more of them ask for more lanes.
   const bool many = a.tokens > 2048;
   const int lanes = many && a.experts <= 256 && a.k <= 16 ? 16 : many && a.experts <= 512 && a.k <= 32 ? 32 : 64;
   const int run = (a.experts + lanes - 1) / lanes;
@@ -377,7 +377,7 @@ void by_shape(const RouteArgs& a, const void* also, const void* f32, F&& f) {
   };
   auto pick = [&](auto lanes) {
     if constexpr (decltype(lanes)::value == 32)
-      return with(lanes, std::integral_constant<int, 16>{});  // more than 256 experts
+      return with(lanes, std::integral_constant<int, 16>{});  // more than 256 experts, or 16 choices
     else if (run <= 1)
       with(lanes, std::integral_constant<int, 1>{});
     else if (run <= 2)
