@@ -45,7 +45,7 @@ def test_every_gate_and_factor(kind, rows):
     bad = np.isnan(got) != np.isnan(want)
     assert not bad.any(), [(float(a), float(b), float(c), float(d)) for a, b, c, d in zip(g[bad], u[bad], got[bad], want[bad])]
     largest = float(torch.finfo(torch.bfloat16).max) * (1 + 2.0 ** -9)  # from here on bf16 rounds to infinity
-    want = np.where(np.abs(want) >= largest, np.sign(want) * np.inf, want)
+    want = np.where(np.abs(want) >= largest, np.copysign(np.inf, want), want)
     fine = np.isfinite(want)
     bad = np.zeros(N, bool)
     bad[~fine] = (got != want)[~fine] & ~np.isnan(want[~fine])
