@@ -551,6 +551,104 @@ int moe_q8_gated(const void* xq, const float* x_scale, int64_t x_rows, const int
                  void* stream);
 
 /* ---------------------------------------------------------------------------
+ * What trains a layer of experts: the 16-bit products and their gradients, the
+ * gated activation, the combine's gradient, and the norm of all gradients.  They
+ * behave as the operators above do.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * The experts' products of 16-bit rows and weights, summed in fp32:
+ *   out[i, n] = bf16( sum_k x[r, k] * w[e, n, k] )
+ * for row i of expert e, r = row_index[i] (r = i without row_index):
+ *   x [x_rows, in_features], w [experts, out_features, in_features], out [rows, out_features], all bf16.
+ * expert_offsets (device, as moe_group writes it) gives each expert its rows; rows at or past
+ * expert_offsets[experts] are not written.  Without it (NULL) experts has to be 1 and every row is
+ * its.  row_index holds `rows` entries (moe_group's row_token); an entry outside [0, x_rows) makes its
+ * row of out NaN.  Without row_index x_rows has to be at least rows.
+ * in_features and out_features: multiples of 8, at most 2^20; experts: at most 1024; with row_index
+ * x_rows * in_features below 2^31.
+ */
+int moe_product(const void* x, int64_t x_rows, const int32_t* row_index, const int32_t* expert_offsets, int32_t experts,
+                const void* w, int64_t rows, int32_t in_features, int32_t out_features, void* out, void* stream);
+
+/*
+ * Gradient of moe_product's out by its rows:
+ *   dx[i, k] = bf16( sum_n dy[i, n] * w[e, n, k] )
+ * dy [rows, out_features], dx [rows, in_features] bf16, w and the rows' division as above.  With a
+ * row_index dx is the gradient of row row_index[i] by way of row i; moe_combine adds up a token's.
+ */
+int moe_product_dx(const void* dy, const int32_t* expert_offsets, int32_t experts, const void* w, int64_t rows,
+                   int32_t in_features, int32_t out_features, void* dx, void* stream);
+
+/*
+ * Gradient of moe_product's out by the weights:
+ *   dw[e, n, k] = sum over the rows i of expert e: dy[i, n] * x[r, k]
+ * in fp32, in an order that the sizes alone decide.  dw [experts, out_features, in_features] is of
+ * `dw_type` MOE_TYPE_F32 or _BF16; an expert without rows gets zeros.  With accumulate = 1 (fp32 only) the
+ * sum is added to what dw holds.  A row_index entry of an expert's row outside [0, x_rows) makes the expert's
+ * dw NaN.
+ * `workspace` holds at least moe_product_dw_workspace(rows, experts, in_features, out_features) bytes
+ * (16-byte aligned; 0 where the weights have enough tiles, then NULL will do).
+ */
+int64_t moe_product_dw_workspace(int64_t rows, int32_t experts, int32_t in_features, int32_t out_features);
+int moe_product_dw(const void* dy, const void* x, int64_t x_rows, const int32_t* row_index, const int32_t* expert_offsets,
+                   int32_t experts, int64_t rows, int32_t in_features, int32_t out_features, void* dw, int32_t dw_type,
+                   int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The gated activation of rows that hold g and u side by side, as a product with the gate's and the up
+ * weights one after another leaves them: gu [rows, 2 ffn] bf16, g the first ffn of a row;
+ *   act = bf16( silu(g) * u )                     act [rows, ffn] bf16
+ * and its gradient, with s = 1 / (1 + e^-g):
+ *   dgu = bf16( dact * u * s * (1 + g * (1 - s)) ), bf16( dact * silu(g) )       dgu [rows, 2 ffn] bf16
+ * dgu may be gu itself.  moe_gate_backward's act (optional) is moe_gate's again, for a program that does
+ * not keep it.  expert_offsets (optional, device, [experts + 1]): rows at or past expert_offsets[experts]
+ * are neither read nor written.  ffn: a multiple of 8, at most 2^19.
+ */
+int moe_gate(const void* gu, const int32_t* expert_offsets, int32_t experts, int64_t rows, int32_t ffn, void* act,
+             void* stream);
+int moe_gate_backward(const void* gu, const void* dact, const int32_t* expert_offsets, int32_t experts, int64_t rows,
+                      int32_t ffn, void* dgu, void* act, void* stream);
+
+/*
+ * Gradients of moe_combine's out by recv and by gate:
+ *   drecv[slot[t, j], :] = bf16( gate[t, j] * dout[t, :] )
+ *   dgate[t, j] = sum_h dout[t, h] * recv[slot[t, j], h]       (fp32)
+ *   dout [tokens, hidden], recv and drecv [recv_rows, hidden] bf16, slot [tokens, k] int32, gate and dgate
+ *   [tokens, k] fp32; drecv or dgate may be NULL.
+ * A slot outside [0, recv_rows) has no row: its dgate is 0.  Rows of drecv that no slot names are not
+ * written.  A row that one token names more than once gets the sum of its gates.  Different tokens have
+ * different rows, as in moe_group's slot; a row that two of them named would get the gradient of either.
+ * hidden: a multiple of 8, at most 65536; k: at most 64.
+ */
+int moe_combine_backward(const void* dout, const void* recv, int64_t recv_rows, int32_t hidden, const int32_t* slot,
+                         const float* gate, int64_t tokens, int32_t k, void* drecv, float* dgate, void* stream);
+
+/* A tensor of a list; the list itself is host memory, read by the call. */
+typedef struct {
+  const void* data;   /* device, aligned to its elements; NULL without any                    */
+  void* out;          /* moe_clip: where the scaled tensor goes, data itself for in place     */
+  int64_t count;      /* elements, >= 0                                                       */
+  int32_t type;       /* MOE_TYPE_F32 or _BF16, of data and out                               */
+  int32_t reserved;   /* 0                                                                    */
+} moe_tensor_t;
+
+/*
+ * The norm of many tensors taken as one vector, and their scaling to at most a given norm:
+ *   moe_squares   total = sum over all tensors of v^2          (fp64, in a fixed order)
+ *   moe_clip      norm = sqrt(total),  out = v * max_norm / norm where norm > max_norm, else v
+ * total and norm (fp32, optional) are device memory.  Between the two calls a program with tensors on other
+ * ranks adds up their totals.  A norm that is not finite leaves every value as it is; the caller sees it in
+ * norm.  max_norm >= 0.  moe_clip's outs may not overlap each other or another tensor's data (MOE_EINVAL);
+ * tensors that are their own out are not touched where nothing is scaled.
+ * `workspace` holds at least moe_squares_workspace(tensors, n) bytes (8-byte aligned).
+ */
+int64_t moe_squares_workspace(const moe_tensor_t* tensors, int32_t n);
+int moe_squares(const moe_tensor_t* tensors, int32_t n, double* total, void* workspace, int64_t workspace_bytes,
+                void* stream);
+int moe_clip(const moe_tensor_t* tensors, int32_t n, const double* total, float max_norm, float* norm, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Host-only plan inspection (no GPU needed).  Builds exactly the plan that
  * moe_stage_run would use for these arguments and lets the caller read its
  * tables, so the layout, schedule and combine plan can be checked on a CPU.

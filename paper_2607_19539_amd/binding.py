@@ -35,7 +35,9 @@ EXPORTED = ["moe_stage_create", "moe_stage_run", "moe_stage_run_serial", "moe_st
             "moe_plan_free", "moe_combine", "moe_stage_run_devplan", "moe_stage_run_serial_devplan",
             "moe_stage_plan_info", "moe_stage_plan_copy", "moe_stage_records", "moe_stage_run_serial_static",
             "moe_norm", "moe_norm_backward", "moe_norm_backward_workspace", "moe_q8_rows", "moe_q8_restore", "moe_route",
-            "moe_route_backward", "moe_group", "moe_group_workspace", "moe_q8_product", "moe_q8_gated"]
+            "moe_route_backward", "moe_group", "moe_group_workspace", "moe_q8_product", "moe_q8_gated", "moe_product",
+            "moe_product_dx", "moe_product_dw", "moe_product_dw_workspace", "moe_gate", "moe_gate_backward",
+            "moe_combine_backward", "moe_squares", "moe_squares_workspace", "moe_clip"]
 MOE_STATIC_SCRATCH_BYTES = 64 * 1024 * 1024
 MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
 MOE_TYPE_F32, MOE_TYPE_BF16 = 0, 1
@@ -52,6 +54,11 @@ class moe_route_config_t(ctypes.Structure):
     _fields_ = [("experts", ctypes.c_int32), ("k", ctypes.c_int32), ("groups", ctypes.c_int32),
                 ("top_groups", ctypes.c_int32), ("group_best", ctypes.c_int32), ("score", ctypes.c_int32),
                 ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class moe_tensor_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class moe_stage_stats_t(ctypes.Structure):
@@ -174,8 +181,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.moe_q8_gated.argtypes = [vp, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, i32, i32, vp, vp]
     lib.moe_norm_backward_workspace.argtypes, lib.moe_group_workspace.argtypes = [i64, i32], [i64, i32]
     lib.moe_norm_backward_workspace.restype = lib.moe_group_workspace.restype = i64
+    lib.moe_product.argtypes = [vp, i64, vp, vp, i32, vp, i64, i32, i32, vp, vp]
+    lib.moe_product_dx.argtypes = [vp, vp, i32, vp, i64, i32, i32, vp, vp]
+    lib.moe_product_dw.argtypes = [vp, vp, i64, vp, vp, i32, i64, i32, i32, vp, i32, i32, vp, i64, vp]
+    lib.moe_product_dw_workspace.argtypes, lib.moe_squares_workspace.argtypes = [i64, i32, i32, i32], [vp, i32]
+    lib.moe_product_dw_workspace.restype = lib.moe_squares_workspace.restype = i64
+    lib.moe_gate.argtypes = [vp, vp, i32, i64, i32, vp, vp]
+    lib.moe_gate_backward.argtypes = [vp, vp, vp, i32, i64, i32, vp, vp, vp]
+    lib.moe_combine_backward.argtypes = [vp, vp, i64, i32, vp, vp, i64, i32, vp, vp, vp]
+    lib.moe_squares.argtypes = [vp, i32, vp, vp, i64, vp]
+    lib.moe_clip.argtypes = [vp, i32, vp, f32, vp, vp]
     for name in ("moe_norm", "moe_norm_backward", "moe_q8_rows", "moe_q8_restore", "moe_route", "moe_route_backward",
-                 "moe_group", "moe_q8_product", "moe_q8_gated"):
+                 "moe_group", "moe_q8_product", "moe_q8_gated", "moe_product", "moe_product_dx", "moe_product_dw", "moe_gate",
+                 "moe_gate_backward", "moe_combine_backward", "moe_squares", "moe_clip"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("moe_combine", "moe_stage_create", "moe_stage_run", "moe_stage_run_serial", "moe_stage_query",
                  "moe_stage_times", "moe_stage_destroy", "moe_plan_build", "moe_plan_info"):
@@ -443,9 +461,11 @@ def moe_combine(recv, slot, gate, out, bad_slots=None, stream=None) -> int:
 # ----------------------------------------------------------------------------- operators around the stage
 
 # What a tensor argument may hold (tensor_args.cpp has the same numbers): bf16 or its int16 bit patterns, int8,
-# int32, fp32, bf16 alone, fp32 or bf16.
-_BITS16, _INT8, _INT32, _F32, _BF16, _LOGITS = range(6)
-_KIND_NAMES = ("bf16", "int8", "int32", "float32", "bfloat16", "float32 or bfloat16")
+# int32, fp32, bf16 alone, fp32 or bf16, fp64.  With _HERE the tensor also has to be on the current device.
+_BITS16, _INT8, _INT32, _F32, _BF16, _LOGITS, _F64 = range(7)
+_HERE = 16
+_BITS16_HERE, _INT32_HERE, _F32_HERE, _LOGITS_HERE, _F64_HERE = (k + _HERE for k in (_BITS16, _INT32, _F32, _LOGITS, _F64))
+_KIND_NAMES = ("bf16", "int8", "int32", "float32", "bfloat16", "float32 or bfloat16", "float64")
 ARGS_PATH = os.path.join(PKG, "_lib", "_moe_args.so")
 
 
@@ -454,14 +474,14 @@ def _refuse(name, t, shape, kind):
     if not hasattr(t, "data_ptr"):
         raise ValueError(f"{name} must be a device tensor, got {type(t).__name__}")
     dtypes = {_BITS16: ("bfloat16", "int16"), _INT8: ("int8",), _INT32: ("int32",), _F32: ("float32",),
-              _BF16: ("bfloat16",), _LOGITS: ("float32", "bfloat16")}[kind]
+              _BF16: ("bfloat16",), _LOGITS: ("float32", "bfloat16"), _F64: ("float64",)}[kind % _HERE]
     if str(t.dtype)[6:] not in dtypes or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)} of {_KIND_NAMES[kind]}, got {list(t.shape)} of {t.dtype}")
-    raise ValueError(f"{name} must be a contiguous device tensor")
+        raise ValueError(f"{name} must be {list(shape)} of {_KIND_NAMES[kind % _HERE]}, got {list(t.shape)} of {t.dtype}")
+    raise ValueError(f"{name} must be a contiguous device tensor" + (" on the current device" if kind >= _HERE else ""))
 
 
 def _load_args():
-    global _want, _opt
+    global _want, _opt, _table
     if not os.path.exists(ARGS_PATH):
         raise RuntimeError(f"extension not built: {ARGS_PATH} (run `python -m paper_2607_19539_amd.build`)")
     import torch  # noqa: F401  (the extension uses its libraries)
@@ -471,7 +491,7 @@ def _load_args():
     mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_moe_args", loader))
     loader.exec_module(mod)
     mod.set_refuse(_refuse)
-    _want, _opt = mod.want, mod.opt
+    _want, _opt, _table = mod.want, mod.opt, mod.table
 
 
 def _want(name, t, shape, kind):
@@ -484,6 +504,12 @@ def _opt(name, t, shape, kind):
     """The same of an optional argument: None for None."""
     _load_args()
     return _opt(name, t, shape, kind)
+
+
+def _table(tensors, outs):
+    """A moe_tensor_t for each tensor, as bytes; None if one of them (or its out) will not do."""
+    _load_args()
+    return _table(tensors, outs)
 
 
 def _rows_of(name, t):
@@ -611,6 +637,121 @@ def moe_q8_gated(xq, x_scale, w1, w1_scale, w3, w3_scale, out, row_index=None, e
     lead, mats, tail = _q8_operands(xq, x_scale, w1, w1_scale, out, row_index, expert_offsets, "w1")
     more = (_want("w3", w3, w1.shape, _INT8), _want("w3_scale", w3_scale, w1_scale.shape, _F32))
     return _check(load().moe_q8_gated(*lead, *mats, *more, *tail, _stream_ptr(stream)))
+
+
+def _matrices(name, t):
+    if len(t.shape) != 3:
+        raise ValueError(f"{name} must have three dimensions, got {list(t.shape)}")
+    return t.shape
+
+
+def _offsets(expert_offsets, E):
+    if expert_offsets is None and E != 1:
+        raise ValueError("expert_offsets is needed with more than one expert")
+    return _opt("expert_offsets", expert_offsets, (E + 1,), _INT32_HERE)
+
+
+def moe_product(x, w, out, row_index=None, expert_offsets=None, stream=None) -> int:
+    """out [rows, N] bf16: rows x [n, K] bf16 (taken through row_index, where given) times each expert's weights
+    w [E, N, K] bf16; expert_offsets [E + 1] divides the rows."""
+    n, K = _rows_of("x", x)
+    rows, N = _rows_of("out", out)
+    E = _matrices("w", w)[0]
+    if row_index is None and n < rows:
+        raise ValueError(f"x must have at least out's {rows} rows, got {n}")
+    off = _offsets(expert_offsets, E)
+    return _check(load().moe_product(
+        _want("x", x, (n, K), _BITS16_HERE), n, _opt("row_index", row_index, (rows,), _INT32_HERE), off, E,
+        _want("w", w, (E, N, K), _BITS16_HERE), rows, K, N, _want("out", out, (rows, N), _BITS16_HERE), _stream_ptr(stream)))
+
+
+def moe_product_dx(dy, w, dx, expert_offsets=None, stream=None) -> int:
+    """Gradient of moe_product's out by its rows: dx [rows, K] bf16 from dy [rows, N] and w [E, N, K]."""
+    rows, N = _rows_of("dy", dy)
+    E, _, K = _matrices("w", w)
+    off = _offsets(expert_offsets, E)
+    return _check(load().moe_product_dx(
+        _want("dy", dy, (rows, N), _BITS16_HERE), off, E, _want("w", w, (E, N, K), _BITS16_HERE), rows, K, N,
+        _want("dx", dx, (rows, K), _BITS16_HERE), _stream_ptr(stream)))
+
+
+def moe_product_dw(dy, x, dw, row_index=None, expert_offsets=None, accumulate=False, workspace=None, stream=None) -> int:
+    """Gradient of moe_product's out by the weights: dw [E, N, K] fp32 or bf16 from dy [rows, N] and x [n, K] (through
+    row_index, where given); with ``accumulate`` it is added to what dw (fp32) holds."""
+    rows, N = _rows_of("dy", dy)
+    n, K = _rows_of("x", x)
+    E = _matrices("dw", dw)[0]
+    if row_index is None and n < rows:
+        raise ValueError(f"x must have at least dy's {rows} rows, got {n}")
+    kind = MOE_TYPE_BF16 if dw.element_size() == 2 else MOE_TYPE_F32
+    lib, off = load(), _offsets(expert_offsets, E)
+    args = (_want("dy", dy, (rows, N), _BITS16_HERE), _want("x", x, (n, K), _BITS16_HERE), n,
+            _opt("row_index", row_index, (rows,), _INT32_HERE), off, E, rows, K, N,
+            _want("dw", dw, (E, N, K), _LOGITS_HERE), kind, int(bool(accumulate)))
+    ws, size = _workspace(workspace, lib.moe_product_dw_workspace(rows, E, K, N), stream)
+    return _check(lib.moe_product_dw(*args, ws if ws is None else ws.data_ptr(), size, _stream_ptr(stream)))
+
+
+def _gate_rows(gu, expert_offsets):
+    rows, F2 = _rows_of("gu", gu)
+    if F2 % 2:
+        raise ValueError(f"gu must hold as many gate as up values, got rows of {F2}")
+    E = 0 if expert_offsets is None else expert_offsets.shape[0] - 1
+    return rows, F2 // 2, _opt("expert_offsets", expert_offsets, (E + 1,), _INT32_HERE), E
+
+
+def moe_gate(gu, act, expert_offsets=None, stream=None) -> int:
+    """act [rows, F] bf16 = silu(g) * u of rows gu [rows, 2 F] that hold g and u side by side; rows at or past the last
+    of expert_offsets are left alone."""
+    rows, F, off, E = _gate_rows(gu, expert_offsets)
+    return _check(load().moe_gate(_want("gu", gu, (rows, 2 * F), _BITS16_HERE), off, E, rows, F,
+                                  _want("act", act, (rows, F), _BITS16_HERE), _stream_ptr(stream)))
+
+
+def moe_gate_backward(gu, dact, dgu, act=None, expert_offsets=None, stream=None) -> int:
+    """Gradient of moe_gate: dgu [rows, 2 F] bf16 (gu itself will do) from dact [rows, F]; act, where given, is
+    written again."""
+    rows, F, off, E = _gate_rows(gu, expert_offsets)
+    return _check(load().moe_gate_backward(
+        _want("gu", gu, (rows, 2 * F), _BITS16_HERE), _want("dact", dact, (rows, F), _BITS16_HERE), off, E, rows, F,
+        _want("dgu", dgu, (rows, 2 * F), _BITS16_HERE), _opt("act", act, (rows, F), _BITS16_HERE), _stream_ptr(stream)))
+
+
+def moe_combine_backward(dout, recv, slot, gate, drecv=None, dgate=None, stream=None) -> int:
+    """Gradients of moe_combine: drecv [rows, H] bf16 and dgate [T, k] fp32 from dout [T, H] and the call's recv, slot
+    and gate."""
+    T, H = _rows_of("dout", dout)
+    rows, _ = _rows_of("recv", recv)
+    _, k = _rows_of("slot", slot)
+    return _check(load().moe_combine_backward(
+        _want("dout", dout, (T, H), _BITS16_HERE), _want("recv", recv, (rows, H), _BITS16_HERE), rows, H,
+        _want("slot", slot, (T, k), _INT32_HERE), _want("gate", gate, (T, k), _F32_HERE), T, k,
+        _opt("drecv", drecv, (rows, H), _BITS16_HERE), _opt("dgate", dgate, (T, k), _F32_HERE), _stream_ptr(stream)))
+
+
+def _tensor_list(tensors, out=None):
+    entries = _table(tensors, out)
+    if entries is None:
+        raise ValueError("tensors must be contiguous float32 or bfloat16 tensors on the current device, out as many of the "
+                         "same types and sizes")
+    return entries, len(entries) // ctypes.sizeof(moe_tensor_t)
+
+
+def moe_squares(tensors, total, workspace=None, stream=None) -> int:
+    """total [1] fp64: the sum of the squares of all elements of a list of fp32 or bf16 tensors."""
+    entries, n = _tensor_list(tensors)
+    lib = load()
+    ptr = _want("total", total, (1,), _F64_HERE)
+    ws, size = _workspace(workspace, lib.moe_squares_workspace(entries, n), stream)
+    return _check(lib.moe_squares(entries, n, ptr, ws if ws is None else ws.data_ptr(), size, _stream_ptr(stream)))
+
+
+def moe_clip(tensors, total, max_norm, out=None, norm=None, stream=None) -> int:
+    """Scales the tensors (in place, or into the list ``out``) to a norm of at most ``max_norm``, where ``total`` [1]
+    fp64 is their sum of squares; the norm before it in ``norm`` [1] fp32."""
+    entries, n = _tensor_list(tensors, out)
+    return _check(load().moe_clip(entries, n, _want("total", total, (1,), _F64_HERE), max_norm,
+                                  _opt("norm", norm, (1,), _F32_HERE), _stream_ptr(stream)))
 
 
 def moe_stage_query(h, check: bool = True) -> dict:

@@ -5,6 +5,7 @@ Run as ``python -m paper_2607_19539_amd.build``.  Cross-compiles without a GPU.
 """
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
@@ -16,8 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libmoe_stage.so")
 ARGS_LIB = os.path.join(LIBDIR, "_moe_args.so")
-SOURCES = ["kernels.hip", "combine.hip", "plan_device.hip", "norm.hip", "route.hip", "group.hip", "q8_product.hip", "plan.cpp",
-           "api.cpp", "ops_api.cpp"]
+SOURCES = ["kernels.hip", "combine.hip", "plan_device.hip", "norm.hip", "route.hip", "group.hip", "q8_product.hip", "product.hip",
+           "product_dw.hip", "gate.hip", "combine_backward.hip", "clip.hip", "plan.cpp", "api.cpp", "ops_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # -packed-fp32-ops: never emit packed fp32 VALU ops (v_pk_add/mul/fma_f32).
@@ -29,14 +30,15 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-command-line-argum
 def build(verbose: bool = False) -> str:
     os.makedirs(LIBDIR, exist_ok=True)
     with tempfile.TemporaryDirectory(prefix="moe_build_") as tmp:
-        objs = []
-        for src in SOURCES:
+        def compiled(src):
             obj = os.path.join(tmp, src + ".o")
             # api.cpp holds the no-allocation entry point's device array, so it is HIP source too.
             lang = ["-x", "hip"] if src.endswith(".hip") or src == "api.cpp" else []
-            cmd = [HIPCC, *COMMON, *DEVICE_FLAGS, *lang, "-c", os.path.join(CSRC, src), "-o", obj]
-            _run(cmd, verbose)
-            objs.append(obj)
+            _run([HIPCC, *COMMON, *DEVICE_FLAGS, *lang, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+            return obj
+
+        with concurrent.futures.ThreadPoolExecutor(4) as pool:
+            objs = list(pool.map(compiled, SOURCES))
         out_tmp = LIB + ".tmp"
         _run([HIPCC, *DEVICE_FLAGS, "-shared", "-fPIC", *objs, "-o", out_tmp], verbose)
         os.replace(out_tmp, LIB)

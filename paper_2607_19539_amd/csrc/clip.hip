@@ -1,0 +1,156 @@
+// clip.hip -- gfx950 kernels of the norm of many tensors and of their scaling to at most a given norm.
+//
+//   total = sum over all tensors of v^2;   v *= max_norm / sqrt(total)  where that is below 1
+//
+// Squares are taken and added in 64 bits: no gradient is too large or too small for its square, and the order of the
+// sum does not show in the 32-bit norm.  Memory bounds both passes.  The tensors' addresses travel in the kernel's
+// arguments, so nothing is copied before a launch and a captured launch keeps them.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "launch.hpp"
+#include "ops.hpp"
+#include "vec_device.hpp"
+
+namespace moe {
+
+namespace {
+
+constexpr int kThreads = 256;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// A chunk's tensor: first[] of up to 128 tensors, two a lane.
+struct Place {
+  int tensor;
+  int64_t from, n;  // elements
+};
+__device__ __forceinline__ Place place(const TensorTable& t, uint32_t chunk, uint32_t first0, uint32_t first1) {
+  const int i = __popcll(__ballot(first0 <= chunk)) + __popcll(__ballot(first1 <= chunk)) - 1;
+  Place p;
+  p.tensor = i;
+  p.from = (int64_t)(chunk - t.first[i]) * t.chunk;
+  p.n = min((int64_t)t.chunk, t.count[i] - p.from);
+  return p;
+}
+__device__ __forceinline__ uint32_t first_of(const TensorTable& t, int i) { return i < t.n ? t.first[i] : UINT32_MAX; }
+
+__device__ __forceinline__ float f32_of(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
+// The workgroup's sum, in thread 0 of it.
+template <int kWaves>
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double parts[kWaves];
+  v = wave_reduce(v, [](double x, double y) { return x + y; });
+  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = parts[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) s += parts[w];
+  return s;
+}
+
+// f(vector) of the 16-byte pieces of n elements at p and f(element) of those before the first piece and after the last.
+template <class T, class Vec, class One>
+__device__ __forceinline__ void pieces(const T* p, int64_t n, Vec&& vec, One&& one) {
+  constexpr int kLane = 16 / sizeof(T);
+  const int64_t head = min(n, (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (int64_t)sizeof(T)), whole = (n - head) / kLane;
+  for (int64_t i = threadIdx.x; i < head; i += kThreads) one(i);
+  for (int64_t i = threadIdx.x; i < whole; i += kThreads) vec(head + i * kLane);
+  for (int64_t i = head + whole * kLane + threadIdx.x; i < n; i += kThreads) one(i);
+}
+
+__global__ __launch_bounds__(kThreads) void squares_kernel(TensorTable t, double* parts) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t first0 = first_of(t, lane), first1 = first_of(t, lane + 64);
+  double s0 = 0, s1 = 0;
+  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const Place p = place(t, c, first0, first1);
+    const uint64_t at = t.in[p.tensor];
+    auto add2 = [&](float a, float b) {
+      s0 = fma((double)a, (double)a, s0);
+      s1 = fma((double)b, (double)b, s1);
+    };
+    if (at >> 63) {
+      const uint16_t* v = (const uint16_t*)(at << 1 >> 1) + p.from;
+      pieces(v, p.n, [&](int64_t i) {
+        float f[8];
+        unpack8(*(const u32x4*)(v + i), f);
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) add2(f[q], f[q + 1]);
+      }, [&](int64_t i) { add2(f32_of(v[i]), 0.0f); });
+    } else {
+      const float* v = (const float*)at + p.from;
+      pieces(v, p.n, [&](int64_t i) {
+        const f32x4 f = *(const f32x4*)(v + i);
+        add2(f[0], f[1]);
+        add2(f[2], f[3]);
+      }, [&](int64_t i) { add2(v[i], 0.0f); });
+    }
+  }
+  const double s = block_sum<kThreads / 64>(s0 + s1);
+  if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(1024) void squares_sum_kernel(const double* parts, int n, double* total) {
+  double s = 0;
+  for (int i = threadIdx.x; i < n; i += 1024) s += parts[i];
+  s = block_sum<16>(s);
+  if (threadIdx.x == 0) *total = s;
+}
+
+// Chunks from the last to the first: what the sum of squares has read last is nearest.
+__global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable t, const double* total, float max_norm, float* norm) {
+  const double root = sqrt(*total);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
+  // A norm that is not finite leaves the gradients as they are.
+  const float scale = root > (double)max_norm && root < __builtin_huge_val() ? (float)((double)max_norm / root) : 1.0f;
+  const int lane = threadIdx.x & 63;
+  const uint32_t first0 = first_of(t, lane), first1 = first_of(t, lane + 64);
+  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const Place p = place(t, t.chunks - 1 - c, first0, first1);
+    const uint64_t at = t.in[p.tensor];
+    const bool bf16 = at >> 63;
+    const uint64_t in = at << 1 >> 1, to = t.out[p.tensor];
+    if (in == to && scale == 1.0f) continue;
+    const bool alike = ((in ^ to) & 15) == 0;  // pieces of 16 bytes in both
+    if (bf16) {
+      const uint16_t* v = (const uint16_t*)in + p.from;
+      uint16_t* o = (uint16_t*)to + p.from;
+      auto one = [&](int64_t i) { o[i] = (uint16_t)bf16x2_of(f32_of(v[i]) * scale, 0.0f); };
+      if (alike)
+        pieces(v, p.n, [&](int64_t i) {
+          float f[8];
+          unpack8(*(const u32x4*)(v + i), f);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] *= scale;
+          *(u32x4*)(o + i) = pack8(f);
+        }, one);
+      else
+        for (int64_t i = threadIdx.x; i < p.n; i += kThreads) one(i);
+    } else {
+      const float* v = (const float*)in + p.from;
+      float* o = (float*)to + p.from;
+      auto one = [&](int64_t i) { o[i] = v[i] * scale; };
+      if (alike)
+        pieces(v, p.n, [&](int64_t i) { *(f32x4*)(o + i) = *(const f32x4*)(v + i) * scale; }, one);
+      else
+        for (int64_t i = threadIdx.x; i < p.n; i += kThreads) one(i);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_squares(const TensorTable& t, double* parts, int blocks, hipStream_t s) {
+  return launch(squares_kernel, dim3((uint32_t)blocks), dim3(kThreads), 0, s, t, parts);
+}
+hipError_t launch_squares_sum(const double* parts, int n, double* total, hipStream_t s) {
+  return launch(squares_sum_kernel, dim3(1), dim3(1024), 0, s, parts, n, total);
+}
+hipError_t launch_clip(const TensorTable& t, const double* total, float max_norm, float* norm, int blocks, hipStream_t s) {
+  return launch(clip_kernel, dim3((uint32_t)blocks), dim3(kThreads), 0, s, t, total, max_norm, norm);
+}
+
+}  // namespace moe

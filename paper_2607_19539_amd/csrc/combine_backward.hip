@@ -1,0 +1,82 @@
+// combine_backward.hip -- gfx950 kernel of the combine's gradient.
+//
+//   drecv[slot[t, j]] = bf16( gate[t, j] dout[t] ),   dgate[t, j] = sum_h dout[t, h] recv[slot[t, j], h]
+//
+// A wave takes one choice of one token: it reads dout's row and recv's, and writes drecv's, 16 bytes a lane.  The choices
+// of a token are next to each other, in one workgroup or on one XCD, so that dout's row comes from memory once.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "launch.hpp"
+#include "ops.hpp"
+#include "plan_types.hpp"
+#include "vec_device.hpp"
+
+namespace moe {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineBackwardArgs a, uint32_t per_xcd) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Workgroups b, b + 8, ... share an XCD: each XCD takes a run of choices.
+  const int64_t choice = (int64_t)((blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds) * kWaves + wave;
+  if (blockIdx.x / kXcds >= per_xcd || choice >= a.tokens * a.k) return;
+  const int64_t t = choice / a.k;
+  const int j = (int)(choice % a.k), H = a.H;
+  const int32_t slot = a.slot[choice];
+  if (slot < 0 || slot >= a.recv_rows) {
+    if (a.dgate && lane == 0) a.dgate[choice] = 0.0f;
+    return;
+  }
+  // A row that a token names more than once takes all of its gates, through the first of them.
+  float gate = a.gate[choice];
+  bool write = a.drecv != nullptr;
+  if (a.k > 1 && write) {
+    const uint64_t same = __ballot(lane < a.k && a.slot[t * a.k + min(lane, a.k - 1)] == slot);
+    uint64_t more = same & ~(1ull << j);
+    write = (same & ((1ull << j) - 1)) == 0;
+    for (; more && write; more &= more - 1) gate += a.gate[t * a.k + __builtin_ctzll(more)];
+  }
+  const uint16_t* dout = a.dout + t * H;
+  const uint16_t* recv = a.recv + (int64_t)slot * H;
+  uint16_t* drecv = a.drecv + (int64_t)slot * H;
+  float sum = 0.0f;
+  auto piece = [&](const u32x4& dv, const u32x4& rv, int h) {
+    float d[8], r[8];
+    unpack8(dv, d);
+    unpack8(rv, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sum = fmaf(d[i], r[i], sum);
+      d[i] *= gate;
+    }
+    if (write) *(u32x4*)(drecv + h) = pack8(d);
+  };
+  constexpr int kAhead = 4;  // pieces in flight
+  int h = lane * 8;
+  for (; h + (kAhead - 1) * 512 < H; h += kAhead * 512) {
+    u32x4 d[kAhead], r[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) d[u] = *(const u32x4*)(dout + h + u * 512), r[u] = *(const u32x4*)(recv + h + u * 512);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) piece(d[u], r[u], h + u * 512);
+  }
+  for (; h < H; h += 512) piece(*(const u32x4*)(dout + h), *(const u32x4*)(recv + h), h);
+  if (a.dgate) {
+    sum = wave_reduce(sum, [](float x, float y) { return x + y; });
+    if (lane == 0) a.dgate[choice] = sum;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s) {
+  const int64_t blocks = (a.tokens * a.k + kWaves - 1) / kWaves, per_xcd = (blocks + kXcds - 1) / kXcds;
+  if (!launch_fits(per_xcd * kXcds, kThreads)) return hipErrorInvalidConfiguration;
+  return launch(combine_backward_kernel, dim3((uint32_t)(per_xcd * kXcds)), dim3(kThreads), 0, s, a, (uint32_t)per_xcd);
+}
+
+}  // namespace moe

@@ -1,6 +1,7 @@
-// mma_tile.hpp -- device code: the K loops of the matrix products, shared by the bf16 producer and the
-// 8-bit products.  An operand row gives 128 bytes to each K step, whatever its type, so the two differ in
-// the matrix instruction alone (Op), and in where K may end (Tail).
+// mma_tile.hpp -- device code: the K loops of the matrix products, shared by the bf16 producer, the 8-bit
+// products and the bf16 products and their gradients.  An operand row gives 128 bytes to each K step, whatever its
+// type, so they differ in the matrix instruction alone (Op), in how an operand lies in memory (layouts) and in where
+// K may end (Tail).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -44,6 +45,36 @@ __device__ __forceinline__ int item_thread() {
   int t = threadIdx.x;
   asm volatile("" : "+v"(t));
   return t;
+}
+
+// How an operand lies in its block.  A block row is 128 bytes, a matrix instruction's fragment of a lane 16: eight
+// 2-byte k of output row (or column) lane % 16, those from 8 (lane / 16) on of a 32-deep sub-step.
+//
+// ByRow: block row r holds the K step's k of output row r, so a fragment is one chunk.
+struct ByRow {
+  static constexpr bool transposed = false;
+};
+// ByK, of 2-byte elements whose rows in memory are k (a matrix that is multiplied from its other side): panels of
+// 64 output rows, in each 64 block rows, one for each k of the step.  ds_read_b64_tr_b16 turns them round as they are
+// read: 16 lanes read 4 k by 16 output rows, lane t 8 bytes of k t / 4, and get the 4 k of output row t.  The 32
+// lanes of a half wave read 32 bytes of 8 block rows, k0 .. k0 + 3 and k0 + 8 .. k0 + 11; chunks are stored at
+// c ^ swz_k(k), which spreads those over all 64 banks (two of the block rows fill them).
+struct ByK {
+  static constexpr bool transposed = true;
+};
+__device__ __forceinline__ uint32_t swz_k(uint32_t k) { return (k & 2u) | ((k >> 1) & 4u); }
+
+// An accumulator's word.  As assembly: left to itself the compiler copies whole accumulators to vector registers
+// ahead of their use, and spills.
+__device__ __forceinline__ int acc_read(int v) {
+  int r;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(v));
+  return r;
+}
+__device__ __forceinline__ float acc_read(float v) {
+  float r;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(v));
+  return r;
 }
 
 // Calls f(integral_constant<int, 0>) .. f(integral_constant<int, n - 1>).
@@ -110,12 +141,86 @@ struct DmaRows {
   uint32_t off[kDma];
 };
 
+// An operand ByK whose k are rows of a matrix that an index names, the item's from index[0] on.  Block row i of the K
+// step is k, and a lane's DMAs take those from `first` on, 8 apart.  The wave holds the rows of up to eight K steps, a
+// k a lane, and passes a step's around as it comes: the load behind them makes the compiler wait for every DMA as
+// well, which it cannot count, once in eight steps.
+constexpr int kIndexSteps = 8;
+template <int kDma>
+struct IndexedRows {
+  const uint8_t* base;       // at the tile's first output row
+  uint32_t off[kDma];
+  const int32_t* index;
+  int n;                     // entries of index
+  uint32_t limit, stride;    // of the matrix: rows, and bytes of one
+  uint32_t chunk[2];         // the lane's chunk in even and odd DMAs
+  int first;                 // block row of the lane's first DMA
+  bool bad;                  // an entry outside the matrix was met (its row 0 is taken instead)
+  int32_t ahead[kIndexSteps];
+  __device__ __forceinline__ void to(int step) {
+    const int lane = (int)(threadIdx.x & 63);
+    if (step % kIndexSteps == 0) {
+      // The last step starts early, as ElementTail has it, or repeats the last row.
+#pragma unroll
+      for (int u = 0; u < kIndexSteps; ++u) ahead[u] = index[min(min((step + u) * kTileK, max(n - kTileK, 0)) + lane, n - 1)];
+      // All of them are waited for here: later waits for one each would wait for the DMAs between them.
+#pragma unroll
+      for (int u = 0; u < kIndexSteps; ++u) asm volatile("" : "+v"(ahead[u]));
+    } else {
+#pragma unroll
+      for (int u = 0; u + 1 < kIndexSteps; ++u) ahead[u] = ahead[u + 1];
+    }
+    bad |= (uint32_t)ahead[0] >= limit;
+    const int row = (uint32_t)ahead[0] < limit ? ahead[0] : 0;
+#pragma unroll
+    for (int q = 0; q < kDma; ++q)
+      off[q] = (uint32_t)__builtin_amdgcn_ds_bpermute((first + 8 * q) * 4, row) * stride + chunk[q & 1];
+  }
+};
+
 // Byte offset from the operand rows' start of lane l's chunk of tile row n = first + l / 8, for rows
 // of `stride` bytes of which row `row` (relative to the base) feeds tile row n: chunk c of a row is
 // stored at c ^ swz(n), so the lane at slot l % 8 fetches chunk (l % 8) ^ swz(n).
 __device__ __forceinline__ uint32_t dma_off(uint32_t n, uint32_t row, uint32_t stride, int lane) {
   return row * stride + (((uint32_t)(lane & 7) ^ swz(n)) << 4);
 }
+
+// A wave's fragments of an operand: those of the 16 output rows from d on of the operand's, of sub-step kk of the
+// K step in ring slot `slot`.  `first` is the wave's first output row, a multiple of 32.
+template <class Layout, class Frag>
+struct Fragments;
+template <class Frag>
+struct Fragments<ByRow, Frag> {
+  uint32_t base;
+  explicit __device__ __forceinline__ Fragments(uint32_t first, int lane) {
+    // The lane reads logical chunk 4kk + lk of its row, stored at chunk (4kk + lk) ^ swz = (lk ^ swz) ^ 4kk: one base
+    // per operand and sub-step, the slot added, and the 16-row block an immediate offset.  (Rows of fragment bases,
+    // multiples of 16, + lr share lr's swizzle.)
+    const uint32_t lr = lane & 15, lk = lane >> 4;
+    base = first * kRowBytes + lr * kRowBytes + ((lk ^ swz(lr)) << 4);
+  }
+  __device__ __forceinline__ Frag read(const uint8_t* lds, uint32_t slot, int kk, int d) const {
+    return *(const Frag*)(lds + ((base ^ ((uint32_t)kk << 6)) + slot + d * kRowBytes));
+  }
+};
+template <class Frag>
+struct Fragments<ByK, Frag> {
+  uint32_t base;
+  explicit __device__ __forceinline__ Fragments(uint32_t first, int lane) {
+    // k = 32kk + 8lk + 4h + lr / 4: its bits 1 and 3, all that swz_k takes, are the lane's alone.  The 16-row block
+    // within a panel (d / 16 % 4) is two bits of the chunk, and so is that of `first`.
+    const uint32_t lr = lane & 15, lk = lane >> 4, k = 8 * lk + (lr >> 2);
+    const uint32_t c = swz_k(k) ^ (((first >> 4) & 3u) << 1);
+    base = (first >> 6) * (64 * kRowBytes) + k * kRowBytes + ((c | ((lr & 3u) >> 1)) << 4) + ((lr & 1u) << 3);
+  }
+  __device__ __forceinline__ Frag read(const uint8_t* lds, uint32_t slot, int kk, int d) const {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    const uint8_t* p = lds + ((base ^ (((uint32_t)d & 48u) << 1)) + slot) + (d >> 6) * (64 * kRowBytes) + kk * (32 * kRowBytes);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)LDS_PTR(p));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)LDS_PTR(p + 4 * kRowBytes));
+    return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
 
 // ---------------------------------------------------------------------------
 // The matrix instruction is v_mfma_f32_16x16x32_bf16.  At these sizes the chip is limited by its
@@ -163,6 +268,27 @@ struct ChunkTail {  // int8
     lo = (int)back / 16;
     hi = K >= kRowBytes ? 8 : K / 16;
   }
+  __device__ __forceinline__ uint32_t back_w() const { return back; }
+  __device__ __forceinline__ uint32_t back_x() const { return back; }
+};
+// ElementTail: at any element of 2 bytes.  The last K step starts `back` elements early, where K is a whole number of
+// chunks and fills a step, so that no row is read past its end; else the lanes past the end read something else of
+// the operand.  Elements outside [lo, hi) are zeroed in both operands, since either may hold infinities there.
+struct ElementTail {
+  static constexpr bool partial = true;
+  static __device__ __forceinline__ int steps(int K) { return (K + kTileK - 1) / kTileK; }
+  uint32_t bytes_w, bytes_x;
+  int lo, hi;
+  // step_w, step_x: bytes from one k to the next of each operand.
+  __device__ __forceinline__ ElementTail(int K, bool early, uint32_t step_w, uint32_t step_x) {
+    const int rest = K % kTileK, back = early && K >= kTileK && rest ? kTileK - rest : 0;
+    bytes_w = (uint32_t)back * step_w;
+    bytes_x = (uint32_t)back * step_x;
+    lo = back;
+    hi = back || !rest ? kTileK : rest;
+  }
+  __device__ __forceinline__ uint32_t back_w() const { return bytes_w; }
+  __device__ __forceinline__ uint32_t back_x() const { return bytes_x; }
 };
 
 // Sub-step kk of a partial last K step: weight fragments of chunks that it does not hold become zeros.  A
@@ -170,7 +296,7 @@ struct ChunkTail {  // int8
 // compiler does not see to for assembly.
 template <class Tail, class Frag, int kNI>
 __device__ __forceinline__ void mask_chunks(const Tail& tail, int kk, int lk, Frag (&fa)[kNI]) {
-  if constexpr (Tail::partial) {
+  if constexpr (std::is_same_v<Tail, ChunkTail>) {
     if (tail.lo > 0 || tail.hi < 8) {
       const int c = 4 * kk + lk;
       const bool keep = c >= tail.lo && c < tail.hi;
@@ -183,17 +309,58 @@ __device__ __forceinline__ void mask_chunks(const Tail& tail, int kk, int lk, Fr
   }
 }
 
-// Moves both operands' bases to K step `next` of nk, one step on (none before the first).
-template <int kDmaW, int kDmaX, class Tail>
-__device__ __forceinline__ void advance_to(DmaRows<kDmaW>& w, DmaRows<kDmaX>& x, int next, int nk, const Tail& tail) {
+// Fragments first .. first + n - 1 of either operand in sub-step kk of an ElementTail's last K step; the other tails
+// need none of it.
+template <class Tail, class Frag, int kN>
+__device__ __forceinline__ void mask_elements(const Tail& tail, int kk, int lk, Frag (&f)[kN], int first, int n) {
+  if constexpr (std::is_same_v<Tail, ElementTail>) {
+    if (tail.lo > 0 || tail.hi < kTileK) {
+      typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+      u32x4_t keep;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int k = 32 * kk + 8 * lk + 2 * q;
+        keep[q] = (k >= tail.lo && k < tail.hi ? 0xFFFFu : 0u) | (k + 1 >= tail.lo && k + 1 < tail.hi ? 0xFFFF0000u : 0u);
+      }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        if (i < first || i >= first + n) continue;
+        f[i] = __builtin_bit_cast(Frag, __builtin_bit_cast(u32x4_t, f[i]) & keep);
+        asm volatile("s_nop 1" : "+v"(f[i]));
+      }
+    }
+  }
+}
+
+// An operand's source at K step `next`, one step on from where it was.
+template <int kDma>
+__device__ __forceinline__ void next_step(DmaRows<kDma>& r, int) {
+  r.base += r.step;
+}
+template <int kDma>
+__device__ __forceinline__ void next_step(IndexedRows<kDma>& r, int next) {
+  r.to(next);
+}
+
+// A last K step that starts early.
+template <int kDma>
+__device__ __forceinline__ void start_early(DmaRows<kDma>& r, uint32_t bytes) {
+  r.base -= bytes;
+}
+template <int kDma>
+__device__ __forceinline__ void start_early(IndexedRows<kDma>&, uint32_t) {}  // as its rows say
+
+// Moves both operands to K step `next` of nk, one step on (none before the first).
+template <class W, class X, class Tail>
+__device__ __forceinline__ void advance_to(W& w, X& x, int next, int nk, const Tail& tail) {
   if (next > 0) {
-    w.base += w.step;
-    x.base += x.step;
+    next_step(w, next);
+    next_step(x, next);
   }
   if constexpr (Tail::partial) {
     if (next == nk - 1) {
-      w.base -= tail.back;
-      x.base -= tail.back;
+      start_early(w, tail.back_w());
+      start_early(x, tail.back_x());
     }
   }
 }
@@ -231,19 +398,18 @@ __device__ __forceinline__ void mfma_drain(Acc (&acc)[kNI][kNJ]) {
 // ---------------------------------------------------------------------------
 
 // The DMAs of a K step: weights to lds_w, tokens to lds_x (this wave's parts of their blocks).
-template <int kDmaW, int kDmaX>
-__device__ __forceinline__ void fetch_step(const DmaRows<kDmaW>& w, const DmaRows<kDmaX>& x, uint32_t lds_w, uint32_t lds_x) {
-  static_for<kDmaW>([&](auto q) {
+template <class W, class X>
+__device__ __forceinline__ void fetch_step(const W& w, const X& x, uint32_t lds_w, uint32_t lds_x) {
+  static_for<sizeof(w.off) / 4>([&](auto q) {
     dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w);
   });
-  static_for<kDmaX>([&](auto q) { dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x); });
+  static_for<sizeof(x.off) / 4>([&](auto q) { dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x); });
 }
 
 // Prologue: K steps 0 and 1 in flight.  w.base and x.base then point at the next step to fetch.  The ring has to be
 // free; nothing is waited for, so the DMAs may run under what the caller does before tile_run.
-template <int kNJ, class Tail>
-__device__ __forceinline__ void tile_start(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
-                                           const Tail& tail) {
+template <int kNJ, class W, class Tail>
+__device__ __forceinline__ void tile_start(uint8_t* __restrict__ lds, W& w, DmaRows<kNJ>& x, int K, const Tail& tail) {
   const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
   const int nk = Tail::steps(K);
   const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
@@ -259,17 +425,17 @@ __device__ __forceinline__ void tile_start(uint8_t* __restrict__ lds, DmaRows<kD
 
 // The K loop after tile_start: late() two K steps (or one) before the end, last() before the last step, when every
 // DMA has arrived.
-template <class Op, int kNJ, class Tail, class Late, class Last>
-__device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
-                                         const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Late&& late, Last&& last) {
+template <class Op, class LayoutW = ByRow, class LayoutX = ByRow, int kNJ, class W, class Tail, class Late, class Last>
+__device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRows<kNJ>& x, int K, const Tail& tail,
+                                         typename Op::Acc (&acc)[8][kNJ], Late&& late, Last&& last) {
   typedef typename Op::Frag Frag;
   static_assert(kNJ == 4 || kNJ == 6 || kNJ == 8, "token fragments per wave");
+  static_assert(!LayoutX::transposed || kNJ != 6, "a wave's tokens start on half a panel or on a panel");
   constexpr int kHJ = kNJ / 2;
   const int tid = item_thread(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave & 1, wm = wave >> 1;
-  const int lr = lane & 15, lk = lane >> 4;
-  const uint32_t lsw = swz(lr);  // rows of fragment bases (multiples of 16) + lr share lr's swizzle
+  const int lk = lane >> 4;
 
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -282,19 +448,11 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, DmaRows<kDma
   // Ring slots by block: o0, o1 hold K step ks's weights and tokens, o2 and o3 step ks+1's, o4 takes
   // step ks+2's weights and o0, once read, its tokens.  They rotate by two per step.
   uint32_t o0 = 0, o1 = kBlockBytes, o2 = 2 * kBlockBytes, o3 = 3 * kBlockBytes, o4 = 4 * kBlockBytes;
-  // Fragments of sub-step kk: the lane reads logical chunk 4kk + lk of its row, stored at chunk
-  // (4kk + lk) ^ lsw = (lk ^ lsw) ^ 4kk: one base per operand and sub-step, the slot added, and the
-  // 16-row block an immediate offset.
-  const uint32_t lane_chunk = (uint32_t)lr * kRowBytes + (((uint32_t)lk ^ lsw) << 4);
-  const uint32_t a_lane = (uint32_t)(wn * 128) * kRowBytes + lane_chunk;
-  const uint32_t b_lane = (uint32_t)(wm * 16 * kNJ) * kRowBytes + lane_chunk;
+  const Fragments<LayoutW, Frag> a_lane((uint32_t)(wn * 128), lane);
+  const Fragments<LayoutX, Frag> b_lane((uint32_t)(wm * 16 * kNJ), lane);
   Frag fa[8], fb[kNJ];
-  auto read_a = [&](uint32_t slot, int kk, int i) {
-    fa[i] = *(const Frag*)(lds + ((a_lane ^ ((uint32_t)kk << 6)) + slot + i * 16 * kRowBytes));
-  };
-  auto read_b = [&](uint32_t slot, int kk, int j) {
-    fb[j] = *(const Frag*)(lds + ((b_lane ^ ((uint32_t)kk << 6)) + slot + j * 16 * kRowBytes));
-  };
+  auto read_a = [&](uint32_t slot, int kk, int i) { fa[i] = a_lane.read(lds, slot, kk, i * 16); };
+  auto read_b = [&](uint32_t slot, int kk, int j) { fb[j] = b_lane.read(lds, slot, kk, j * 16); };
 
   // Step 0 visible, its first sub-step read.
   if (nk > 1)
@@ -355,11 +513,24 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, DmaRows<kDma
     using steady = std::integral_constant<bool, kd == 0>;
     using first = std::integral_constant<int, 0>;
     using second = std::integral_constant<int, 1>;
-    if constexpr (kd == 2) mask_chunks(tail, 0, lk, fa);
+    // In the last step, the elements that it does not hold: of what half 0 multiplies, then of half 1's.
+    auto mask0 = [&](int kk) {
+      if constexpr (kd == 2) {
+        mask_chunks(tail, kk, lk, fa);
+        mask_elements(tail, kk, lk, fa, 0, 8);
+        mask_elements(tail, kk, lk, fb, 0, kHJ);
+      }
+    };
+    auto mask1 = [&](int kk) {
+      if constexpr (kd == 2) mask_elements(tail, kk, lk, fb, kHJ, kHJ);
+    };
+    mask0(0);
     half0(first{}, steady{});
+    mask1(0);
     half1(o0, o1, second{}, std::true_type{}, steady{});
-    if constexpr (kd == 2) mask_chunks(tail, 1, lk, fa);
+    mask0(1);
     half0(second{}, std::false_type{});
+    mask1(1);
     if constexpr (kd < 2) wait_vm_and_barrier<kd == 0 ? kDmaPerThread : 0>();  // step ks+1 visible, step ks's slots free
     half1(o2, o3, first{}, std::integral_constant<bool, (kd < 2)>{}, steady{});
     if constexpr (kd == 0) advance_to(w, x, ks + 3, nk, tail);
@@ -413,7 +584,7 @@ __device__ __forceinline__ void narrow_start(uint8_t* __restrict__ lds, DmaRows<
 }
 
 // The K loop after narrow_start: late() three K steps (or fewer) before the end, last() before the last one's.
-template <class Op, int kNB, class Tail, class Late, class Last>
+template <class Op, class LayoutW = ByRow, int kNB, class Tail, class Late, class Last>
 __device__ __forceinline__ void narrow_run(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNB / 2>& x, int K,
                                            const Tail& tail, typename Op::Acc (&acc)[4][kNB], Late&& late, Last&& last) {
   typedef typename Op::Frag Frag;
@@ -425,11 +596,9 @@ __device__ __forceinline__ void narrow_run(uint8_t* __restrict__ lds, DmaRows<kD
   constexpr int kDmaStage = kDmaPerThread + kDmaX;
   const int tid = item_thread(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 15, lk = lane >> 4;
-  const uint32_t lsw = swz(lr);
-  const uint32_t lane_chunk = (uint32_t)lr * kRowBytes + (((uint32_t)lk ^ lsw) << 4);
-  const uint32_t a_lane = (uint32_t)((wave >> 1) * 128 + (wave & 1) * 32) * kRowBytes + lane_chunk;
-  const uint32_t b_lane = (uint32_t)kBlockBytes + lane_chunk;
+  const int lk = lane >> 4;
+  const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave >> 1) * 128 + (wave & 1) * 32), lane);
+  const Fragments<ByRow, Frag> b_lane(0u, lane);
 
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -455,14 +624,17 @@ __device__ __forceinline__ void narrow_run(uint8_t* __restrict__ lds, DmaRows<kD
     for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
       for (int j = 0; j < kNB; ++j)
-        fb[kk][j] = *(const Frag*)(lds + ((b_lane ^ ((uint32_t)kk << 6)) + st + j * 16 * kRowBytes));
+        fb[kk][j] = b_lane.read(lds, (uint32_t)kBlockBytes + st, kk, j * 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        fa[kk][i] = *(const Frag*)(lds + ((a_lane ^ ((uint32_t)kk << 6)) + st + ((i >> 1) * 64 + (i & 1) * 16) * kRowBytes));
+      for (int i = 0; i < 4; ++i) fa[kk][i] = a_lane.read(lds, st, kk, (i >> 1) * 64 + (i & 1) * 16);
     }
     if constexpr (decltype(last)::value) {
-      mask_chunks(tail, 0, lk, fa[0]);
-      mask_chunks(tail, 1, lk, fa[1]);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        mask_chunks(tail, kk, lk, fa[kk]);
+        mask_elements(tail, kk, lk, fa[kk], 0, 4);
+        mask_elements(tail, kk, lk, fb[kk], 0, kNB);
+      }
     }
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
@@ -500,6 +672,93 @@ __device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kD
                                            int K, const Tail& tail, typename Op::Acc (&acc)[4][kNB], Late&& late) {
   narrow_start<kNB>(lds, w, x, K, tail);
   narrow_run<Op>(lds, w, x, K, tail, acc, late, [] {});
+}
+
+// ---------------------------------------------------------------------------
+// kW weight rows by kX rows in two by two waves, for products too small for whole tiles: a ring of four K steps.
+// A step's second half of fragments is read under the products of the first; the barrier between the two ends
+// every wave's reads of the step, whose slot is filled again at once, and the next step's first half is read under
+// the products of the second.
+template <class Op, int kW, int kX, class LayoutW = ByRow, class LayoutX = ByRow, class W, class Tail>
+__device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, W& w, DmaRows<kX / 32>& x, int K, const Tail& tail,
+                                          typename Op::Acc (&acc)[kW / 32][kX / 32]) {
+  typedef typename Op::Frag Frag;
+  constexpr int kStages = 4, kNI = kW / 32, kNJ = kX / 32;
+  constexpr uint32_t kStageBytes = (kW + kX) * kRowBytes;
+  constexpr int kDmaStage = kNI + kNJ;
+  const int tid = item_thread(), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lk = lane >> 4;
+  const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * (kW / 2)), lane);
+  const Fragments<LayoutX, Frag> b_lane((uint32_t)((wave >> 1) * (kX / 2)), lane);
+#pragma unroll
+  for (int i = 0; i < kNI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) acc[i][j] = typename Op::Acc{};
+  const int nk = Tail::steps(K);
+  const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kNI * 1024;
+  const uint32_t lds_x = lds_addr(lds) + kW * kRowBytes + (uint32_t)wave * kNJ * 1024;
+  int loaded = 0;
+  uint32_t st_load = 0, st_use = 0;
+  auto next = [](uint32_t st) { return st == (kStages - 1) * kStageBytes ? 0u : st + kStageBytes; };
+  auto load = [&]() {
+    fetch_step(w, x, lds_w + st_load, lds_x + st_load);
+    advance_to(w, x, ++loaded, nk, tail);
+    st_load = next(st_load);
+  };
+  Frag fa[2][kNI], fb[2][kNJ];
+  auto read = [&](int kk) {
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) fb[kk][j] = b_lane.read(lds, kW * kRowBytes + st_use, kk, j * 16);
+#pragma unroll
+    for (int i = 0; i < kNI; ++i) fa[kk][i] = a_lane.read(lds, st_use, kk, i * 16);
+  };
+  auto multiply = [&](int kk) {
+#pragma unroll
+    for (int i = 0; i < kNI; ++i)
+#pragma unroll
+      for (int j = 0; j < kNJ; ++j) Op::mma(acc[i][j], fa[kk][i], fb[kk][j]);
+  };
+  // ahead: K steps behind the next one that may still be in flight; -1: there is no next step.
+  auto step = [&](auto ahead, auto fetch) {
+    constexpr int n = decltype(ahead)::value;
+    read(1);
+    if constexpr (n < 0) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        mask_chunks(tail, kk, lk, fa[kk]);
+        mask_elements(tail, kk, lk, fa[kk], 0, kNI);
+        mask_elements(tail, kk, lk, fb[kk], 0, kNJ);
+      }
+    }
+    multiply(0);
+    if constexpr (n >= 0) {
+      wait_vm_and_barrier<n * kDmaStage>();
+      st_use = next(st_use);
+      if constexpr (decltype(fetch)::value) load();
+      read(0);
+    }
+    multiply(1);
+  };
+  using std::false_type;
+  advance_to(w, x, 0, nk, tail);
+  for (int ks = 0; ks < min(nk, kStages); ++ks) load();
+  if (nk >= 4)
+    wait_vm_and_barrier<3 * kDmaStage>();
+  else if (nk == 3)
+    wait_vm_and_barrier<2 * kDmaStage>();
+  else if (nk == 2)
+    wait_vm_and_barrier<kDmaStage>();
+  else
+    wait_vm_and_barrier<0>();
+  read(0);
+  for (int ks = 0; ks + kStages < nk; ++ks) step(std::integral_constant<int, 2>{}, std::true_type{});
+  if (nk >= 4) step(std::integral_constant<int, 2>{}, false_type{});
+  if (nk >= 3) step(std::integral_constant<int, 1>{}, false_type{});
+  if (nk >= 2) step(std::integral_constant<int, 0>{}, false_type{});
+  step(std::integral_constant<int, -1>{}, false_type{});
+  mfma_drain(acc);
+  wait_vm_and_barrier<0>();
 }
 
 }  // namespace moe

@@ -78,6 +78,61 @@ struct Q8Args {
   int32_t experts, K, N;
 };
 
+struct ProductArgs {       // out[i, n] = sum_k x[index[i], k] W[n, k]
+  const uint16_t* x;       // [x_rows, K]
+  const int32_t* index;    // [rows] or null
+  const int32_t* offsets;  // [experts + 1] or null (one expert)
+  const uint16_t* w;       // [experts, N, K]; by_k: [experts, K, N]
+  uint16_t* out;           // [rows, N]
+  int64_t x_rows, rows;
+  int32_t experts, K, N;
+};
+
+struct ProductDwArgs {     // dw[e, n, k] = sum over rows i of e: dy[i, n] x[index[i], k]
+  const uint16_t* dy;      // [rows, N]
+  const uint16_t* x;       // [x_rows, K]
+  const int32_t* index;    // [rows] or null
+  const int32_t* offsets;  // [experts + 1] or null (one expert)
+  void* dw;                // [experts, N, K]
+  float* parts;            // [split, experts, N, K] where the rows are split
+  int64_t x_rows, rows;
+  int32_t experts, K, N;
+  int32_t bf16, accumulate;
+};
+
+struct GateArgs {
+  const uint16_t* gu;      // [rows, 2 F]
+  const uint16_t* dact;    // [rows, F]
+  uint16_t* act;           // [rows, F]
+  uint16_t* dgu;           // [rows, 2 F]
+  const int32_t* end;      // rows at or past *end are left alone; null: none are
+  int64_t rows;
+  int32_t F;
+};
+
+struct CombineBackwardArgs {
+  const uint16_t* dout;  // [tokens, H]
+  const uint16_t* recv;  // [recv_rows, H]
+  const int32_t* slot;   // [tokens, k]
+  const float* gate;     // [tokens, k]
+  uint16_t* drecv;       // [recv_rows, H]
+  float* dgate;          // [tokens, k] or null
+  int64_t tokens, recv_rows;
+  int32_t k, H;
+};
+
+// Up to kTableTensors tensors as a kernel's argument.  Their elements are taken in chunks, numbered through.
+constexpr int kTableTensors = 128;
+struct TensorTable {
+  uint64_t in[kTableTensors];     // address; the top bit marks bf16 (fp32 otherwise)
+  uint64_t out[kTableTensors];
+  int64_t count[kTableTensors];   // elements, none of them 0
+  uint32_t first[kTableTensors];  // the tensor's first chunk
+  uint32_t chunk, chunks;         // elements of a chunk, a multiple of 8; chunks there are
+  int32_t n;
+};
+static_assert(sizeof(TensorTable) <= 3840, "a kernel's arguments have 4 KiB");
+
 // A launch has fewer than 2^32 threads; one that would need more is refused with hipErrorInvalidConfiguration.
 constexpr bool launch_fits(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
 
@@ -97,5 +152,25 @@ enum Q8Kind { kQ8Slim1, kQ8Slim2, kQ8Tiles64, kQ8Tiles128, kQ8Tiles256 };
 Q8Kind q8_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool gated);
 hipError_t launch_q8_kind(Q8Kind kind, const Q8Args& a, bool gated, hipStream_t s);
 hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s);
+
+// Which kernel takes a 16-bit product: 16 rows by 16 or 32 features straight from memory, or tiles of 64, 128 or 256
+// features by as many rows through LDS.  by_k: W's columns lie in memory, not its rows.
+enum ProductKind { kProductSlim1, kProductSlim2, kProductTiles64, kProductTiles128, kProductTiles256 };
+ProductKind product_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool by_k);
+hipError_t launch_product_kind(ProductKind kind, const ProductArgs& a, bool by_k, hipStream_t s);
+hipError_t launch_product(const ProductArgs& a, bool by_k, hipStream_t s);
+// How the weights' gradient is computed: tiles of 64, 128 or 256 each way, an expert's rows in so many parts.
+struct DwPlan {
+  int tile, split;
+};
+DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N);
+hipError_t launch_product_dw_plan(const DwPlan& plan, const ProductDwArgs& a, hipStream_t s);
+hipError_t launch_gate(const GateArgs& a, hipStream_t s);
+hipError_t launch_gate_backward(const GateArgs& a, hipStream_t s);
+// parts: a sum of each of the `blocks` workgroups.
+hipError_t launch_squares(const TensorTable& t, double* parts, int blocks, hipStream_t s);
+hipError_t launch_squares_sum(const double* parts, int n, double* total, hipStream_t s);
+hipError_t launch_clip(const TensorTable& t, const double* total, float max_norm, float* norm, int blocks, hipStream_t s);
+hipError_t launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s);
 
 }  // namespace moe

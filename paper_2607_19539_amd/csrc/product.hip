@@ -1,0 +1,472 @@
+// product.hip -- gfx950 kernels of the experts' 16-bit products and of the gradient by their rows.
+//
+//   moe_product     out[i, n] = bf16( sum_k x[r_i, k] w[e, n, k] )
+//   moe_product_dx  dx[i, k]  = bf16( sum_n dy[i, n] w[e, n, k] )
+//
+// Both are out[i, n] = sum_k x[r_i, k] W[n, k], with W's rows in memory (ByRow) or its columns (ByK: the LDS read turns
+// them round, so the weights are needed once and in one layout).  v_mfma_f32_16x16x32_bf16, sums in fp32.  The weights
+// are the A operand, so a lane ends up with 4 consecutive features of one row and stores them together.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "expert_tiles.hpp"
+#include "launch.hpp"
+#include "mma_tile.hpp"
+#include "ops.hpp"
+#include "vec_device.hpp"
+
+namespace moe {
+
+namespace {
+
+template <bool by_k>
+using WeightLayout = std::conditional_t<by_k, ByK, ByRow>;
+
+constexpr float kNan = __builtin_nanf("");
+
+// Where a K loop over a.K ends: rows of a.K elements are not read past their end.
+template <bool by_k>
+__device__ __forceinline__ ElementTail tail_of(const ProductArgs& a) {
+  return ElementTail(a.K, true, by_k ? (uint32_t)a.N * 2 : 2u, 2u);
+}
+
+// The weights of a tile as a DMA source: kDma instructions a wave, the tile's features from `first` on.
+template <bool by_k, int kDma>
+__device__ __forceinline__ void weight_rows(const ProductArgs& a, int expert, int first, int lane, int wave, DmaRows<kDma>& w) {
+  const int K = a.K, N = a.N;
+  const uint32_t r8 = (uint32_t)lane >> 3;
+  if constexpr (by_k) {
+    // Block rows of the wave's DMAs: panel by panel, 64 k each.
+    const int panel = wave * kDma / 8, k0 = wave * kDma % 8 * 8;
+    w.step = (uint32_t)kTileK * (uint32_t)N * 2;
+    w.base = (const uint8_t*)(a.w + (int64_t)expert * K * N + first);
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) {
+      const uint32_t k = (uint32_t)(k0 + 8 * i) + r8;
+      const int col = min(first + panel * 64 + (int)((((uint32_t)lane & 7) ^ swz_k(k)) << 3), N - 8) - first;
+      w.off[i] = (min(k, (uint32_t)K - 1) * (uint32_t)N + (uint32_t)col) * 2;
+    }
+  } else {
+    const int cmax = min(K / 8, 8) - 1;
+    auto feature = [&](int n) { return min(first + n, N - 1); };
+    const int f0 = feature(wave * kDma * 8);
+    w.step = kRowBytes;
+    w.base = (const uint8_t*)(a.w + ((int64_t)expert * N + f0) * K);
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) {
+      const uint32_t n = (uint32_t)((wave * kDma + i) * 8) + r8;
+      const uint32_t c = min(((uint32_t)lane & 7) ^ swz(n), (uint32_t)cmax);
+      w.off[i] = (uint32_t)(feature((int)n) - f0) * (uint32_t)K * 2 + (c << 4);
+    }
+  }
+}
+
+// Whether row i of out has a row of x, and which; a row that row_index does not name takes row 0 (any readable one).
+__device__ __forceinline__ bool named(const ProductArgs& a, uint32_t r) { return (int64_t)r < a.x_rows; }
+
+// ------------------------------------------------------------------------------------ small tiles
+
+template <int kW, int kX>
+struct SmallShape {
+  static constexpr int kStride = kW * 2 + 16;  // of a finished row in LDS
+  static constexpr int kOutBytes = kX * kStride;
+};
+
+// One tile of kW features by kX rows, of which it.rows are valid.
+template <bool by_k, int kW, int kX>
+__device__ __forceinline__ void small_item(const ProductArgs& a, const Item& it, uint8_t* lds) {
+  using S = SmallShape<kW, kX>;
+  constexpr int kNI = kW / 32, kNJ = kX / 32;
+  const int tid = item_thread(), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lk = lane >> 4;
+  const int K = a.K, N = a.N, first = it.col * kW;
+  const uint32_t cmax = (uint32_t)min(K / 8, 8) - 1;
+  DmaRows<kNI> w;
+  DmaRows<kNJ> x;
+  weight_rows<by_k>(a, it.expert, first, lane, wave, w);
+  auto source = [&](int m) {
+    const int i = it.row0 + min(m, it.rows - 1);
+    return (uint32_t)(a.index ? a.index[i] : i);
+  };
+  const int row0 = a.index ? 0 : it.row0;
+  x.step = kRowBytes;
+  x.base = a.x_rows > 0 ? (const uint8_t*)(a.x + (int64_t)row0 * K) : (const uint8_t*)a.w;
+#pragma unroll
+  for (int i = 0; i < kNJ; ++i) {
+    const uint32_t n = (uint32_t)((wave * kNJ + i) * kRowsPerDma) + ((uint32_t)lane >> 3), r = source((int)n);
+    const uint32_t c = min(((uint32_t)lane & 7) ^ swz(n), cmax);
+    x.off[i] = (named(a, r) ? (r - (uint32_t)row0) * (uint32_t)K * 2 : 0u) + (c << 4);
+  }
+  bool ok[kNJ];
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) ok[j] = !a.index || named(a, source((wave >> 1) * (kX / 2) + j * 16 + lr));
+  // Offsets are complete before the first operand DMA, which the compiler does not count.
+#pragma unroll
+  for (int i = 0; i < kNJ; ++i) asm volatile("" ::"v"(x.off[i]));
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) asm volatile("" ::"v"((int)ok[j]));
+
+  f32x4 acc[kNI][kNJ];
+  small_mma<Bf16Mma, kW, kX, WeightLayout<by_k>>(lds, w, x, K, tail_of<by_k>(a), acc);
+
+#pragma unroll
+  for (int i = 0; i < kNI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      f32x4 v = acc[i][j];
+      if (!ok[j]) v = f32x4{kNan, kNan, kNan, kNan};
+      const int m = (wave >> 1) * (kX / 2) + j * 16 + lr, n = (wave & 1) * (kW / 2) + i * 16 + 4 * lk;
+      *(u32x2*)(lds + m * S::kStride + n * 2) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
+    }
+  __syncthreads();
+  constexpr int kLanes = kW / 8;  // threads that store one row
+  const int c8 = tid % kLanes, f = first + c8 * 8;
+  if (f < N) {
+#pragma unroll 4
+    for (int p = 0; p < kX * kLanes / kThreads; ++p) {
+      const int m = p * (kThreads / kLanes) + tid / kLanes;
+      if (m < it.rows) *(u32x4*)(a.out + (int64_t)(it.row0 + m) * N + f) = *(const u32x4*)(lds + m * S::kStride + c8 * 16);
+    }
+  }
+}
+
+template <bool by_k, int kW, int kX>
+__global__ __launch_bounds__(kThreads, kW + kX <= 128 ? 2 : 1) void product_small_kernel(ProductArgs a, int cols) {
+  constexpr int kRing = 4 * (kW + kX) * kRowBytes, kOut = SmallShape<kW, kX>::kOutBytes;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing > kOut ? kRing : kOut];
+  const Item it = uniform(Items<kX>(a, cols).find(a, blockIdx.x % kXcds, blockIdx.x / kXcds));
+  if (it.rows <= 0) return;
+  small_item<by_k, kW, kX>(a, it, lds);
+}
+
+// ------------------------------------------------------------------------------------ whole tiles
+
+// What a tile's DMAs read.
+template <bool by_k>
+struct ProductSource {
+  DmaRows<kDmaPerThread> w;
+  DmaRows<8> x;
+  // First the rows, which may have to be looked up ...
+  __device__ __forceinline__ void rows(const ProductArgs& a, const Item& it) {
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const int dx = row_dmas(it.rows);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int n = (wave * dx + i) * kRowsPerDma + (lane >> 3), m = it.row0 + min(n, it.rows - 1);
+      x.off[i] = (uint32_t)(a.index ? a.index[m] : m);
+    }
+  }
+  // ... then the addresses.
+  __device__ __forceinline__ void addresses(const ProductArgs& a, const Item& it) {
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const int K = a.K, dx = row_dmas(it.rows);
+    const uint32_t cmax = (uint32_t)min(K / 8, 8) - 1;
+    weight_rows<by_k>(a, it.expert, it.col * 256, lane, wave, w);
+    const int row0 = a.index ? 0 : it.row0;
+    x.step = kRowBytes;
+    x.base = a.x_rows > 0 ? (const uint8_t*)(a.x + (int64_t)row0 * K) : (const uint8_t*)a.w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t r = x.off[i], n = (uint32_t)((wave * dx + i) * kRowsPerDma) + ((uint32_t)lane >> 3);
+      const uint32_t c = min(((uint32_t)lane & 7) ^ swz(n), cmax);
+      x.off[i] = (named(a, r) ? (r - (uint32_t)row0) * (uint32_t)K * 2 : 0u) + (c << 4);
+      asm volatile("" ::"v"(x.off[i]));  // complete before the first DMA, which the compiler does not count
+    }
+  }
+  template <int kDma>
+  __device__ __forceinline__ DmaRows<kDma> first_rows() const {
+    DmaRows<kDma> r{x.base, x.step, {}};
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) r.off[i] = x.off[i];
+    return r;
+  }
+  // The first K steps on their way, the bases at the step after them.
+  __device__ __forceinline__ void start(const ProductArgs& a, const Item& it, uint8_t* lds) {
+    const ElementTail tail = tail_of<by_k>(a);
+    auto narrow = [&](auto dma) {
+      auto r = first_rows<decltype(dma)::value>();
+      narrow_start<2 * decltype(dma)::value>(lds, w, r, a.K, tail);
+      x.base = r.base;
+    };
+    auto tall = [&](auto dma) {
+      auto r = first_rows<decltype(dma)::value>();
+      tile_start<decltype(dma)::value>(lds, w, r, a.K, tail);
+      x.base = r.base;
+    };
+    using std::integral_constant;
+    switch (row_dmas(it.rows)) {
+      case 1: return narrow(integral_constant<int, 1>{});
+      case 2: return narrow(integral_constant<int, 2>{});
+      case 4: return tall(integral_constant<int, 4>{});
+      case 6: return tall(integral_constant<int, 6>{});
+      default: return tall(integral_constant<int, 8>{});
+    }
+  }
+};
+
+// The K loop and the epilogue of a tile of 32 kDma rows by 256 features, whose first K steps `src` has started.
+// Between the two the next item's are started, so that they arrive under the epilogue, which keeps to registers.
+template <bool by_k, int kDma>
+__device__ __forceinline__ void tile_item(const ProductArgs& a, const Item& it, const Item& next, ProductSource<by_k>& src, uint8_t* lds) {
+  constexpr bool kNarrow = kDma <= 2;             // four waves by the features alone
+  constexpr int kNI = kNarrow ? 4 : 8;            // weight fragments per wave
+  constexpr int kNJ = kNarrow ? 2 * kDma : kDma;  // row fragments per wave
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  const int N = a.N;
+  auto quad_n = [&](int i) {
+    return kNarrow ? (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16 : (wave & 1) * 128 + i * 16;
+  };
+  auto quad_m = [&](int j, int lane) { return (kNarrow ? 0 : (wave >> 1) * (16 * kNJ)) + j * 16 + (lane & 15); };
+  const int first = it.col * 256;
+  DmaRows<kDma> x = src.template first_rows<kDma>();
+  f32x4 acc[kNI][kNJ];
+  const ElementTail tail = tail_of<by_k>(a);
+  // Which rows there are, and the next item's, are asked for near the loop's end: all are there when it ends, and no
+  // wait for them meets a DMA.
+  uint32_t r[kNJ];
+  auto late = [&] {
+    const int lane = item_thread() & 63;
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      const int m = it.row0 + min(quad_m(j, lane), it.rows - 1);
+      r[j] = (uint32_t)(a.index ? a.index[m] : m);
+    }
+    if (next.rows > 0) src.rows(a, next);
+  };
+  if constexpr (kNarrow)
+    narrow_run<Bf16Mma, WeightLayout<by_k>>(lds, src.w, x, a.K, tail, acc, late, [] {});
+  else
+    tile_run<Bf16Mma, WeightLayout<by_k>>(lds, src.w, x, a.K, tail, acc, late, [] {});
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) asm volatile("" ::"v"(r[j]));
+  if (next.rows > 0) {
+    src.addresses(a, next);
+    src.start(a, next, lds);
+  }
+  const int lane = item_thread() & 63, lk = lane >> 4;
+  // A lane has 4 consecutive features of a row in each of two fragments; the lanes 16 apart exchange quads, so that
+  // each stores 8 consecutive features of one.
+#pragma unroll
+  for (int i = 0; i < kNI; i += 2) {
+    const int f = first + quad_n(i) + (lk & 1) * 16 + (lk >> 1) * 8;
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) {
+      uint32_t h[2][2];
+      const bool ok = named(a, r[j]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = acc_read(acc[i + u][j][q]);
+          if (!ok) v[q] = kNan;
+        }
+        h[u][0] = bf16x2_of(v[0], v[1]);
+        h[u][1] = bf16x2_of(v[2], v[3]);
+      }
+      const auto lo = __builtin_amdgcn_permlane16_swap(h[0][0], h[1][0], false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(h[0][1], h[1][1], false, false);
+      const int m = quad_m(j, lane);
+      if (m < it.rows && f < N) *(u32x4*)(a.out + (int64_t)(it.row0 + m) * N + f) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
+    }
+  }
+}
+
+// Workgroups that stay: b takes item (b / 8 + 7 n) mod (workgroups of its XCD) of the n-th set that its XCD's
+// workgroups take together.  (Rotating keeps a workgroup from meeting the short last tile of one expert after
+// another.)
+template <bool by_k>
+__global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int cols) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
+  const Items<256> items(a, cols);
+  const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, set = gridDim.x / kXcds;
+  uint32_t n = 0;
+  Item it = uniform(items.find(a, xcd, mine));
+  if (it.rows <= 0) return;
+  ProductSource<by_k> src;
+  src.rows(a, it);
+  src.addresses(a, it);
+  src.start(a, it, lds);
+  while (it.rows > 0) {
+    ++n;
+    const Item next = uniform(items.find(a, xcd, n * set + (mine + 7 * n) % set));
+    switch (row_dmas(it.rows)) {
+      case 1: tile_item<by_k, 1>(a, it, next, src, lds); break;
+      case 2: tile_item<by_k, 2>(a, it, next, src, lds); break;
+      case 4: tile_item<by_k, 4>(a, it, next, src, lds); break;
+      case 6: tile_item<by_k, 6>(a, it, next, src, lds); break;
+      default: tile_item<by_k, 8>(a, it, next, src, lds); break;
+    }
+    it = next;
+  }
+}
+
+// ------------------------------------------------------------------------------------ few rows
+
+// A tile of 16 rows by 16 kN features: the four waves take every fourth 128 bytes of K each, straight from memory
+// into registers, so nothing in the loop waits for another wave, and add their sums up in LDS at the end.
+template <int kN>
+__global__ __launch_bounds__(kThreads) void product_slim_kernel(ProductArgs a) {
+  constexpr int kWaves = kThreads / 64, kStep = 64;  // k of a wave's turn: two of the matrix instruction
+  __shared__ f32x4 sums[kWaves][kN][64];
+  const Item it = uniform(find_rows<16>(a, blockIdx.y));
+  if (it.rows <= 0) return;
+  const int lane = threadIdx.x & 63, lr = lane & 15, lk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int K = a.K, N = a.N, n0 = blockIdx.x * 16 * kN;
+  const uint16_t* wp[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i) wp[i] = a.w + ((int64_t)it.expert * N + min(n0 + i * 16 + lr, N - 1)) * K + lk * 8;
+  const int mine = it.row0 + min(lr, it.rows - 1);
+  const uint32_t r = (uint32_t)(a.index ? a.index[mine] : mine);
+  const bool ok = named(a, r);
+  const uint16_t* xp = (ok ? a.x + (int64_t)r * K : a.w) + lk * 8;
+  f32x4 acc[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i) acc[i] = f32x4{};
+  struct Chunk {
+    bf16x8 w[2][kN], x[2];
+  };
+  auto load = [&](Chunk& c, int k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) c.w[h][i] = *(const bf16x8*)(wp[i] + k + h * 32);
+      c.x[h] = *(const bf16x8*)(xp + k + h * 32);
+    }
+  };
+  auto multiply = [&](const Chunk& c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c.w[h][i], c.x[h], acc[i], 0, 0, 0);
+  };
+  const int nfull = K / kStep;
+  Chunk c0, c1;
+  int c = wave;
+  if (c < nfull) load(c0, c * kStep);
+  while (c < nfull) {
+    if (c + kWaves < nfull) load(c1, (c + kWaves) * kStep);
+    multiply(c0);
+    c += kWaves;
+    if (c >= nfull) break;
+    if (c + kWaves < nfull) load(c0, (c + kWaves) * kStep);
+    multiply(c1);
+    c += kWaves;
+  }
+  if (K % kStep && wave == nfull % kWaves) {  // the last chunks of 8
+    const int k = nfull * kStep;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = k + h * 32 + lk * 8 < K;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        c0.w[h][i] = bf16x8{};
+        if (in) c0.w[h][i] = *(const bf16x8*)(wp[i] + k + h * 32);
+      }
+      c0.x[h] = bf16x8{};
+      if (in) c0.x[h] = *(const bf16x8*)(xp + k + h * 32);
+    }
+    multiply(c0);
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    if (i % kWaves != wave) continue;
+    const int n = n0 + i * 16 + 4 * lk;
+    if (n >= N || lr >= it.rows) continue;
+    f32x4 s = sums[0][i][lane];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) s += sums[w][i][lane];
+    if (!ok) s = f32x4{kNan, kNan, kNan, kNan};
+    *(u32x2*)(a.out + (int64_t)(it.row0 + lr) * N + n) = u32x2{bf16x2_of(s[0], s[1]), bf16x2_of(s[2], s[3])};
+  }
+}
+
+// ------------------------------------------------------------------------------------ host side
+
+template <int kN>
+hipError_t launch_slim(const ProductArgs& a, hipStream_t s) {
+  const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, 16), cols = ((int64_t)a.N + 16 * kN - 1) / (16 * kN);
+  if (tiles > kSlimTiles || !launch_fits(cols, kThreads)) return hipErrorInvalidConfiguration;
+  return launch(product_slim_kernel<kN>, dim3((uint32_t)cols, (uint32_t)tiles), dim3(kThreads), 0, s, a);
+}
+
+template <bool by_k, int kW, int kX>
+hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
+  const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, kX);
+  const int cols = (a.N + kW - 1) / kW;
+  const int64_t grid = dealt(tiles, cols);
+  if (kW == 256 ? grid > INT32_MAX : !launch_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
+  if constexpr (kW == 256)
+    return launch(product_tile_kernel<by_k>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
+  else
+    return launch(product_small_kernel<by_k, kW, kX>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
+}
+
+}  // namespace
+
+ProductKind product_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool by_k) {
+  // What each kernel would take, in microseconds, from the rows an expert has on average (the host does not know
+  // the offsets): the rounds of tiles over 256 compute units, each so many K steps and something for its start and end;
+  // and the reading of every weight, at the rate in TB/s that the kernel reached where that is all.
+  const double nk = (K + kTileK - 1) / kTileK;
+  const double busy = grouped ? experts * (1.0 - std::pow(1.0 - 1.0 / experts, (double)rows)) : 1.0;
+  const double per = rows / busy, megabytes = busy * N * (2e-6 * K);
+  auto tiles = [&](double x) { return grouped ? busy * (1.0 + std::max(0.0, (per - x / 2) / x)) : std::ceil(rows / x); };
+  auto items = [&](double w, double x) { return tiles(x) * std::ceil(N / w) / 256.0; };
+  auto cost = [&](double work, double rate) { return std::max(work, megabytes / rate) + 0.35 * work; };
+  auto step = [](double h) {
+    return h < 64 ? 0.41 + 0.25 * (h - 32) / 32 : h < 128 ? 0.66 + 0.11 * (h - 64) / 64 : 0.77 + 0.615 * (h - 128) / 128;
+  };
+  const double whole = items(256, 256), half = items(128, 128), quarter = items(64, 64);
+  const double height = std::min(256.0, std::max(32.0, per)), rest = whole - std::floor(whole);
+  double tall = std::floor(whole) * (nk * step(height) + 3.5);
+  if (rest > 0) {
+    const int parts = parts_of((uint32_t)std::ceil(rest * kStaying / kXcds));
+    tall += nk * step(std::max(32.0, std::min(height, 256.0 / parts))) + 5;
+  }
+  ProductKind best = kProductTiles256;
+  double least = cost(1.2 + tall, 4.7);
+  auto consider = [&](ProductKind kind, double c) {
+    if (c < least) best = kind, least = c;
+  };
+  // The small tiles and the slim kernels have a workgroup for each item, and can be too many for one launch.
+  auto launches = [&](int w, int x) { return launch_fits(dealt(most_tiles(rows, grouped, experts, x), (N + w - 1) / w), kThreads); };
+  if (launches(128, 128)) consider(kProductTiles128, cost(1.2 + std::ceil(half) * (nk * 0.48 + 2.8), 4.9));
+  if (launches(64, 64)) consider(kProductTiles64, cost(2.4 + std::max(1.0, quarter) * (nk * 0.21 + 0.9), 5.1));
+  if (!by_k && most_tiles(rows, grouped, experts, 16) <= kSlimTiles && launch_fits(((int64_t)N + 15) / 16, kThreads)) {
+    consider(kProductSlim1, cost(2.4 + nk * std::max(0.12, 0.13 * items(16, 16)), 6.9));
+    consider(kProductSlim2, cost(2.4 + nk * 0.16 * std::max(1.0, items(32, 16)), 6.9));
+  }
+  return best;
+}
+
+hipError_t launch_product_kind(ProductKind kind, const ProductArgs& a, bool by_k, hipStream_t s) {
+  switch (kind) {
+    case kProductSlim1:
+      return by_k ? hipErrorInvalidValue : launch_slim<1>(a, s);
+    case kProductSlim2:
+      return by_k ? hipErrorInvalidValue : launch_slim<2>(a, s);
+    case kProductTiles64:
+      return by_k ? launch_tiles<true, 64, 64>(a, s) : launch_tiles<false, 64, 64>(a, s);
+    case kProductTiles128:
+      return by_k ? launch_tiles<true, 128, 128>(a, s) : launch_tiles<false, 128, 128>(a, s);
+    case kProductTiles256:
+      return by_k ? launch_tiles<true, 256, 256>(a, s) : launch_tiles<false, 256, 256>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_product(const ProductArgs& a, bool by_k, hipStream_t s) {
+  return launch_product_kind(product_kind(a.rows, a.offsets != nullptr, a.experts, a.K, a.N, by_k), a, by_k, s);
+}
+
+}  // namespace moe

@@ -1,0 +1,334 @@
+// product_dw.hip -- gfx950 kernels of the gradient of the experts' 16-bit products by their weights.
+//
+//   dw[e, n, k] = sum over rows i of e: dy[i, n] x[r_i, k]      (added to what dw holds, on request)
+//
+// The rows are what is summed over, and both operands have them as rows in memory: both lie ByK in LDS, x as the A
+// operand, so that a lane ends up with 4 consecutive k of one n.  v_mfma_f32_16x16x32_bf16, sums in fp32.  Each expert
+// has as many rows as it has: a K step that is not full starts early, or, with fewer than 64 rows, repeats the last.
+//
+// Where there are fewer tiles than compute units each expert's rows are split into parts, which leave fp32 sums in the
+// workspace, added up in their order by a second launch: the result does not depend on who came first.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "expert_tiles.hpp"
+#include "launch.hpp"
+#include "mma_tile.hpp"
+#include "ops.hpp"
+#include "vec_device.hpp"
+
+namespace moe {
+
+namespace {
+
+constexpr float kNan = __builtin_nanf("");
+constexpr int kBandTiles = 4;  // tiles of n that take turns on a tile of k
+
+struct DwItem {
+  int expert, part, n0, k0;  // the first feature of dy and of x; expert < 0: no item
+  int row0, rows;            // of the part
+};
+
+// The rows of one expert at a time, from its 64 experts' table.
+struct ExpertRows {
+  Experts<256> table;
+  Before past;
+  int e0 = 0;
+  __device__ __forceinline__ explicit ExpertRows(const ProductDwArgs& a) {
+    if (a.offsets) table = Experts<256>(a, 0, past);
+  }
+  __device__ __forceinline__ void of(const ProductDwArgs& a, int e, int& lo, int& hi) {
+    if (!a.offsets) {
+      lo = 0, hi = (int)a.rows;
+      return;
+    }
+    while (e >= e0 + 64) {  // items come in the experts' order
+      past = table.after(a, e0);
+      e0 += 64;
+      table = Experts<256>(a, e0, past);
+    }
+    lo = __builtin_amdgcn_readlane(table.lo, e - e0);
+    hi = __builtin_amdgcn_readlane(table.hi, e - e0);
+  }
+};
+
+// Item `it` of a launch: the experts one after another, in each the parts, in each bands of kBandTiles tiles of n by
+// all tiles of k, the tiles of a band next to each other.
+template <int kTile>
+__device__ __forceinline__ DwItem dw_item(const ProductDwArgs& a, ExpertRows& experts, int split, uint32_t it) {
+  const uint32_t tn = (uint32_t)(a.N + kTile - 1) / kTile, tk = (uint32_t)(a.K + kTile - 1) / kTile, tiles = tn * tk;
+  const uint32_t slice = it / tiles, q = it % tiles;
+  const int e = (int)(slice / (uint32_t)split), part = (int)(slice % (uint32_t)split);
+  if (e >= a.experts) return DwItem{-1, 0, 0, 0, 0, 0};
+  const uint32_t band = q / (kBandTiles * tk), in = q % (kBandTiles * tk), nb = min((uint32_t)kBandTiles, tn - band * kBandTiles);
+  int lo, hi;
+  experts.of(a, e, lo, hi);
+  // Parts of whole K steps.
+  const int steps = (hi - lo + kTileK - 1) / kTileK, each = (steps + split - 1) / split * kTileK;
+  const int row0 = min(lo + part * each, hi);
+  return DwItem{e, part, (int)(band * kBandTiles + in % nb) * kTile, (int)(in / nb) * kTile, row0, min(each, hi - row0)};
+}
+
+__device__ __forceinline__ DwItem uniform(const DwItem& it) {
+  auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  return DwItem{u(it.expert), u(it.part), u(it.n0), u(it.k0), u(it.row0), u(it.rows)};
+}
+
+// kDma instructions a wave of the rows `it` has in a matrix of `width` columns, from column `first` on.
+template <int kDma>
+__device__ __forceinline__ void rows_by_k(const uint16_t* m, int width, const DwItem& it, int first, int lane, int wave, DmaRows<kDma>& d) {
+  const uint32_t r8 = (uint32_t)lane >> 3;
+  const int panel = wave * kDma / 8, k0 = wave * kDma % 8 * 8;
+  d.step = (uint32_t)kTileK * (uint32_t)width * 2;
+  d.base = (const uint8_t*)(m + (int64_t)it.row0 * width + first);
+#pragma unroll
+  for (int i = 0; i < kDma; ++i) {
+    const uint32_t k = (uint32_t)(k0 + 8 * i) + r8;
+    const int col = min(first + panel * 64 + (int)((((uint32_t)lane & 7) ^ swz_k(k)) << 3), width - 8) - first;
+    d.off[i] = (min(k, (uint32_t)it.rows - 1) * (uint32_t)width + (uint32_t)col) * 2;
+    asm volatile("" ::"v"(d.off[i]));
+  }
+}
+
+// x as the A operand: its rows as they lie, or through row_index.
+template <bool indexed, int kDma>
+using XRows = std::conditional_t<indexed, IndexedRows<kDma>, DmaRows<kDma>>;
+
+template <int kDma>
+__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, DmaRows<kDma>& d) {
+  rows_by_k(a.x, a.K, it, it.k0, lane, wave, d);
+}
+template <int kDma>
+__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, IndexedRows<kDma>& d) {
+  const int panel = wave * kDma / 8;
+  d.base = a.x_rows > 0 ? (const uint8_t*)(a.x + it.k0) : (const uint8_t*)a.dy;
+  d.index = a.index + it.row0;
+  d.n = it.rows;
+  d.limit = (uint32_t)a.x_rows;
+  d.stride = (uint32_t)a.K * 2;
+  d.first = wave * kDma % 8 * 8 + (lane >> 3);
+  d.bad = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t k = (uint32_t)(d.first + 8 * h);
+    const int col = min(it.k0 + panel * 64 + (int)((((uint32_t)lane & 7) ^ swz_k(k)) << 3), a.K - 8) - it.k0;
+    d.chunk[h] = (uint32_t)col * 2;
+  }
+  d.to(0);
+#pragma unroll
+  for (int i = 0; i < kDma; ++i) asm volatile("" ::"v"(d.off[i]));  // complete before the first DMA
+}
+
+// Where the sum over an item's rows ends.  An index starts its last step early by itself.
+template <bool indexed>
+__device__ __forceinline__ ElementTail tail_of(const ProductDwArgs& a, int rows) {
+  return ElementTail(rows, true, indexed ? 0u : (uint32_t)a.K * 2, (uint32_t)a.N * 2);
+}
+
+template <int kDma>
+__device__ __forceinline__ bool any_bad(const DmaRows<kDma>&) { return false; }
+template <int kDma>
+__device__ __forceinline__ bool any_bad(const IndexedRows<kDma>& d) { return __any(d.bad); }
+
+// Four consecutive k of dw[e, n, :], or of a part of it.
+__device__ __forceinline__ void store4(const ProductDwArgs& a, const DwItem& it, int split, int n, int k, f32x4 v) {
+  if (n >= a.N || k >= a.K) return;
+  const int64_t at = ((int64_t)it.expert * a.N + n) * a.K + k;
+  if (split > 1) {
+    *(f32x4*)(a.parts + (int64_t)it.part * a.experts * a.N * a.K + at) = v;
+  } else if (a.bf16) {
+    *(u32x2*)((uint16_t*)a.dw + at) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
+  } else {
+    f32x4* out = (f32x4*)((float*)a.dw + at);
+    if (a.accumulate) v += *out;
+    *out = v;
+  }
+}
+
+// ------------------------------------------------------------------------------------ small tiles
+
+template <bool indexed, int kTile>
+__global__ __launch_bounds__(kThreads, kTile <= 64 ? 2 : 1) void dw_small_kernel(ProductDwArgs a, int split) {
+  constexpr int kN = kTile / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[8 * kTile * kRowBytes];
+  ExpertRows experts(a);
+  const DwItem it = uniform(dw_item<kTile>(a, experts, split, blockIdx.x));
+  if (it.expert < 0) return;
+  const int tid = item_thread(), lane = tid & 63, lr = lane & 15, lk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  f32x4 acc[kN][kN];
+  bool bad = false;
+  if (it.rows > 0) {
+    XRows<indexed, kN> x;
+    DmaRows<kN> y;
+    x_rows(a, it, lane, wave, x);
+    rows_by_k(a.dy, a.N, it, it.n0, lane, wave, y);
+    small_mma<Bf16Mma, kTile, kTile, ByK, ByK>(lds, x, y, it.rows, tail_of<indexed>(a, it.rows), acc);
+    if constexpr (indexed) bad = __syncthreads_or(any_bad(x));  // a wave has met a part of the rows
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) acc[i][j] = f32x4{};
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      f32x4 v = acc[i][j];
+      if (bad) v = f32x4{kNan, kNan, kNan, kNan};
+      store4(a, it, split, it.n0 + (wave >> 1) * (kTile / 2) + j * 16 + lr, it.k0 + (wave & 1) * (kTile / 2) + i * 16 + 4 * lk, v);
+    }
+}
+
+// ------------------------------------------------------------------------------------ whole tiles
+
+template <bool indexed>
+struct DwSource {
+  XRows<indexed, kDmaPerThread> x;
+  DmaRows<8> y;
+  __device__ __forceinline__ void start(const ProductDwArgs& a, const DwItem& it, uint8_t* lds) {
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const ElementTail tail = tail_of<indexed>(a, it.rows);
+    x_rows(a, it, lane, wave, x);
+    if (a.N - it.n0 > 128) {
+      rows_by_k(a.dy, a.N, it, it.n0, lane, wave, y);
+      tile_start<8>(lds, x, y, it.rows, tail);
+    } else {
+      DmaRows<4> half;
+      rows_by_k(a.dy, a.N, it, it.n0, lane, wave, half);
+      tile_start<4>(lds, x, half, it.rows, tail);
+      y.base = half.base;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y.off[i] = half.off[i];
+    }
+  }
+};
+
+// The K loop and the epilogue of a tile of 256 k by 32 kDma n, whose first K steps `src` has started.  The next item's
+// are started between the two.
+template <bool indexed, int kDma>
+__device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, const DwItem& it, const DwItem& next, DwSource<indexed>& src,
+                                             uint8_t* lds) {
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  f32x4 acc[8][kDma];
+  bool bad = false;
+  if (it.rows > 0) {
+    DmaRows<kDma> y{src.y.base, (uint32_t)kTileK * (uint32_t)a.N * 2, {}};
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) y.off[i] = src.y.off[i];
+    tile_run<Bf16Mma, ByK, ByK>(lds, src.x, y, it.rows, tail_of<indexed>(a, it.rows), acc, [] {}, [] {});
+    bad = any_bad(src.x);  // every wave has met every row
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < kDma; ++j) {
+        acc[i][j] = f32x4{};
+        asm volatile("" : "+a"(acc[i][j]));
+      }
+  }
+  if (next.rows > 0) src.start(a, next, lds);
+  const int lane = item_thread() & 63, lr = lane & 15, lk = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < kDma; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f32x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[q] = acc_read(acc[i][j][q]);
+        if (bad) v[q] = kNan;
+      }
+      store4(a, it, split, it.n0 + (wave >> 1) * (16 * kDma) + j * 16 + lr, it.k0 + (wave & 1) * 128 + i * 16 + 4 * lk, v);
+      __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
+    }
+}
+
+// Workgroups that stay, a compute unit each; the 32 of an XCD take runs of consecutive items.
+template <bool indexed>
+__global__ __launch_bounds__(kThreads, 1) void dw_tile_kernel(ProductDwArgs a, int split) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
+  ExpertRows experts(a);
+  const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, set = gridDim.x / kXcds;
+  auto find = [&](uint32_t n) { return uniform(dw_item<256>(a, experts, split, (n * kXcds + xcd) * set + (mine + 7 * n) % set)); };
+  uint32_t n = 0;
+  DwItem it = find(0);
+  DwSource<indexed> src;
+  if (it.rows > 0) src.start(a, it, lds);
+  while (it.expert >= 0) {
+    const DwItem next = find(++n);
+    if (a.N - it.n0 > 128)
+      dw_tile_item<indexed, 8>(a, split, it, next, src, lds);
+    else
+      dw_tile_item<indexed, 4>(a, split, it, next, src, lds);
+    it = next;
+  }
+}
+
+// ------------------------------------------------------------------------------------ parts
+
+// dw from the parts, in their order: four elements a thread.
+__global__ __launch_bounds__(kThreads) void dw_sum_kernel(ProductDwArgs a, int split, int64_t quads) {
+  const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (q >= quads) return;
+  f32x4 v = ((const f32x4*)a.parts)[q];
+  for (int p = 1; p < split; ++p) v += ((const f32x4*)a.parts)[p * quads + q];
+  if (a.bf16) {
+    ((u32x2*)a.dw)[q] = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
+  } else {
+    f32x4* out = (f32x4*)a.dw + q;
+    if (a.accumulate) v += *out;
+    *out = v;
+  }
+}
+
+int64_t dw_items(const DwPlan& p, const ProductDwArgs& a) {
+  return (int64_t)a.experts * p.split * ((a.N + p.tile - 1) / p.tile) * ((a.K + p.tile - 1) / p.tile);
+}
+
+template <bool indexed>
+hipError_t launch_dw(const DwPlan& plan, const ProductDwArgs& a, hipStream_t s) {
+  const int64_t items = dw_items(plan, a);
+  if (items > INT32_MAX - 2 * kStaying || (plan.tile != 256 && !launch_fits(items, kThreads))) return hipErrorInvalidConfiguration;
+  if (plan.tile == 64) return launch(dw_small_kernel<indexed, 64>, dim3((uint32_t)items), dim3(kThreads), 0, s, a, plan.split);
+  if (plan.tile == 128) return launch(dw_small_kernel<indexed, 128>, dim3((uint32_t)items), dim3(kThreads), 0, s, a, plan.split);
+  return launch(dw_tile_kernel<indexed>, dim3((uint32_t)std::min<int64_t>((items + kXcds - 1) / kXcds * kXcds, kStaying)), dim3(kThreads), 0, s,
+                a, plan.split);
+}
+
+}  // namespace
+
+DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N) {
+  // What each way would take, in microseconds, from the rows an expert has on average: rounds of tiles, each so many
+  // K steps and something for its start and its end; parts cost the writing and the reading of their sums.
+  const double nk = std::ceil((double)rows / experts / kTileK), megabytes = (double)experts * N * K * 4e-6;
+  DwPlan best{256, 1};
+  double least = 1e30;
+  auto consider = [&](int tile, double at_once, double step, double fixed) {
+    const double tiles = (double)experts * std::ceil((double)N / tile) * std::ceil((double)K / tile);
+    for (int split = 1; split <= 64; split *= 2) {
+      if (split > 1 && (nk / split < 2 || split * megabytes > 1024)) break;
+      const double cost = std::ceil(tiles * split / at_once) * (std::ceil(nk / split) * step + fixed) + megabytes * split / 4.5 +
+                          (split > 1 ? 4.0 + megabytes * split / 6 : 0);
+      if (cost < least) best = DwPlan{tile, split}, least = cost;
+    }
+  };
+  consider(256, 256, 1.45, 6);
+  consider(128, 256, 0.5, 4);
+  consider(64, 512, 0.25, 3);
+  return best;
+}
+
+hipError_t launch_product_dw_plan(const DwPlan& plan, const ProductDwArgs& a, hipStream_t s) {
+  if (hipError_t e = a.index ? launch_dw<true>(plan, a, s) : launch_dw<false>(plan, a, s)) return e;
+  if (plan.split == 1) return hipSuccess;
+  const int64_t quads = (int64_t)a.experts * a.N * a.K / 4, blocks = (quads + kThreads - 1) / kThreads;
+  if (!launch_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+  return launch(dw_sum_kernel, dim3((uint32_t)blocks), dim3(kThreads), 0, s, a, plan.split, quads);
+}
+
+}  // namespace moe

@@ -26,17 +26,13 @@
 #include <algorithm>
 #include <cmath>
 
+#include "expert_tiles.hpp"
 #include "launch.hpp"
 #include "mma_tile.hpp"
 #include "ops.hpp"
 #include "vec_device.hpp"
 
 namespace moe {
-
-constexpr int kThreads = 256;
-constexpr int kBandRows = 1024;  // rows of the tiles that take turns on one weight tile
-constexpr int kStaying = 256;    // workgroups of the whole tiles' kernel: one takes all of a compute unit's LDS
-constexpr int kDeal = 32;        // consecutive items that one XCD's compute units run at a time
 
 // A workgroup's tile: kW weight rows (features, or as many gate and up features in turn) by up to kX rows.
 // Quarter q of the weight rows is gate (q even) or up (q odd) of the same features, so that a wave, which
@@ -53,258 +49,6 @@ struct Shape {
   }
   static __device__ __forceinline__ bool up(int n) { return gated && (n / (kW / 4)) & 1; }
 };
-
-// silu(g) * u = (g / (1 + e^-g)) u, from a quarter of g, with the hardware's exponential and reciprocal, each within
-// one fp32 ulp.  The exponent t = -g log2(e) is rounded, which would cost e^-g an error of |g| 2^-24; the rounding r is
-// made good in the first order (e^-g (1 + r ln 2)), as a bf16 result that falls the other way may change the row's
-// 8-bit scale after it.  With a quarter of 1 + e^-g, too, the reciprocal is never a subnormal, which the hardware
-// would flush: it is 2^-126 or more, and 0 from t = 128 on, where e^-g is infinite in fp32.  Where t itself overflows
-// r is infinite; its factor is kept near a quarter.  u comes last, as g u may overflow where silu(g) u does not.
-constexpr float kGateShare = 0.25f;
-__device__ __forceinline__ float silu_mul(float quarter_g, float u) {
-  constexpr float kLog2e = 4 * 1.44269504f, kLog2eRest = 4 * 1.92596303e-8f, kLn2 = 0.693147181f;
-  constexpr float kLow = 0.15915494f, kHigh = 0.5f;  // constants that an instruction holds
-  const float t = -quarter_g * kLog2e;
-  const float r = fmaf(-quarter_g, kLog2eRest, fmaf(-quarter_g, kLog2e, -t));
-  const float factor = __builtin_amdgcn_fmed3f(fmaf(r, kLn2 / 4, 0.25f), kLow, kHigh);
-  return quarter_g * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), factor, 0.25f)) * u;
-}
-
-// The parts by rows that each of the last round's tiles is cut into, with `per` of them for the kDeal compute units
-// of an XCD: as many as there are units for, down to 32 rows.
-__host__ __device__ __forceinline__ uint32_t parts_of(uint32_t per) {
-  return per * 8 <= kDeal ? 8 : per * 4 <= kDeal ? 4 : per * 2 <= kDeal ? 2 : 1;
-}
-
-struct Item {
-  int expert, col, rows;  // rows: valid rows of the tile, 0: no item
-  int row0;
-};
-
-// v of the lanes up to each, summed.
-__device__ __forceinline__ uint32_t scan_add(uint32_t v) {
-  auto from = [&](auto ctrl, auto rows) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
-  };
-  using std::integral_constant;
-  v += from(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});  // 1, 2, 4, 8 lanes down within 16
-  v += from(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
-  v += from(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
-  v += from(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
-  v += from(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // lane 15 of a row to the next
-  v += from(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // lane 31 to the upper half
-  return v;
-}
-
-// The rows [lo, hi) of 64 experts from e0 on, an expert a lane, and where the tiles of kTile rows of each end in
-// the running count.  The host cannot check the caller's offsets: they are cut to the rows there are and never
-// fall (`seen`: where the experts before e0 end).
-struct Before {
-  int seen = 0;             // where the experts before these end
-  uint32_t tiles = 0;       // and how many tiles they have
-};
-template <int kTile>
-struct Experts {
-  int lo, hi;
-  uint32_t end;
-  Experts() = default;
-  __device__ __forceinline__ Experts(const Q8Args& a, int e0, const Before& b) {
-    const int seen = b.seen;
-    const int lane = threadIdx.x & 63, e = e0 + lane, rows = (int)a.rows;
-    const bool have = e < a.experts;
-    lo = have ? a.offsets[e] : 0;
-    hi = have ? a.offsets[e + 1] : 0;
-    if (__any(have && (lo < seen || hi < lo || hi > rows))) {
-      int m = have ? min(max(max(lo, hi), seen), rows) : seen;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(m, d);
-        if (lane >= d) m = max(m, o);
-      }
-      const int start = __shfl_up(m, 1);
-      lo = lane == 0 ? min(max(lo, seen), m) : max(start, min(lo, m));
-      hi = m;
-      if (!have) lo = hi;
-    }
-    end = b.tiles + scan_add((uint32_t)(hi - lo + kTile - 1) / kTile);
-  }
-  __device__ __forceinline__ Before after(const Q8Args& a, int e0) const {
-    return Before{__builtin_amdgcn_readlane(hi, min(a.experts - e0, 64) - 1), (uint32_t)__builtin_amdgcn_readlane((int)end, 63)};
-  }
-};
-
-// The items of a launch.  An expert's are bands of kBandRows rows by all columns, the tiles of a band next to
-// each other; they are dealt to the XCDs (workgroups b, b + 8, ... share one) in runs of kDeal, so that the
-// compute units of an XCD read the same few weight and row tiles through its L2 (as the parts of one tile do).
-// Every wave finds an item by itself, 64 experts at a time, a lane each.
-template <int kTile>
-struct Items {
-  using X = Experts<kTile>;
-  X table;  // of up to 64 experts
-  uint32_t total = 0, cols;
-  __device__ __forceinline__ Items(const Q8Args& a, int cols_) : cols((uint32_t)cols_) {
-    if (!a.offsets) {
-      total = (uint32_t)((a.rows + kTile - 1) / kTile) * cols;
-    } else {
-      Before all;  // the tiles of all experts are counted first: the deal goes by their number
-      for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        table = X(a, e0, all);
-        all = table.after(a, e0);
-      }
-      total = all.tiles * cols;
-    }
-  }
-  // Item j of XCD xcd's.  It grows with j, so that an XCD without an item j has none after it.
-  __device__ __forceinline__ Item find(const Q8Args& a, uint32_t xcd, uint32_t j) const {
-    const Item none{0, 0, 0, 0};
-    if constexpr (kTile != 256) {
-      const uint32_t run = min((uint32_t)kDeal, (total + kXcds - 1) / kXcds);
-      const uint32_t it = run ? ((j / run) * kXcds + xcd) * run + j % run : 0;
-      return it < total ? at(a, it) : none;
-    } else {
-      const uint32_t whole = total / kStaying * kStaying;
-      if (j < whole / kXcds) return at(a, ((j / kDeal) * kXcds + xcd) * kDeal + j % kDeal);
-      // The last, partly filled round: its tiles are cut into as many parts by rows as there are compute units for.
-      const uint32_t per = (total - whole + kXcds - 1) / kXcds, in = j - whole / kXcds;
-      const uint32_t parts = parts_of(per);
-      const uint32_t it = whole + xcd * per + in / parts;
-      if (in >= per * parts || it >= total) return none;
-      Item found = at(a, it);
-      const int height = kTile / (int)parts, skip = (int)(in % parts) * height;
-      found.row0 += skip;
-      found.rows = min(found.rows - skip, height);
-      return found;
-    }
-  }
-
- private:
-  __device__ __forceinline__ Item at(const Q8Args& a, uint32_t it) const {
-    if (!a.offsets) return place(0, 0, (int)a.rows, total / cols, it);
-    Item found{0, 0, 0, 0};
-    if (a.experts <= 64) {
-      pick(table, 0, Before{}, it, found);
-      return found;
-    }
-    Before past;
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-      const X x(a, e0, past);
-      if (pick(x, e0, past, it, found)) return found;
-      past = x.after(a, e0);
-    }
-    return found;
-  }
-
-  // Item q of an expert with rows [lo, hi) in `tiles` tiles.
-  __device__ __forceinline__ Item place(int expert, int lo, int hi, uint32_t tiles, uint32_t q) const {
-    constexpr uint32_t kBand = kBandRows / kTile;
-    const uint32_t band = q / (kBand * cols), in = q % (kBand * cols);
-    const uint32_t nb = min(kBand, tiles - band * kBand);
-    const int row0 = lo + (int)(band * kBand + in % nb) * kTile;
-    return Item{expert, (int)(in / nb), min(kTile, hi - row0), row0};
-  }
-  __device__ __forceinline__ bool pick(const X& x, int e0, const Before& b, uint32_t it, Item& found) const {
-    const uint64_t past = __ballot(it < x.end * cols);
-    if (past == 0) return false;
-    const int l = __builtin_ctzll(past);
-    const uint32_t first = l == 0 ? b.tiles : (uint32_t)__builtin_amdgcn_readlane((int)x.end, l - 1);
-    const uint32_t tiles = (uint32_t)__builtin_amdgcn_readlane((int)x.end, l) - first;
-    found = place(e0 + l, __builtin_amdgcn_readlane(x.lo, l), __builtin_amdgcn_readlane(x.hi, l), tiles, it - first * cols);
-    return true;
-  }
-};
-
-// The item in scalar registers: it is the same in every lane.
-__device__ __forceinline__ Item uniform(const Item& it) {
-  return Item{__builtin_amdgcn_readfirstlane(it.expert), __builtin_amdgcn_readfirstlane(it.col),
-              __builtin_amdgcn_readfirstlane(it.rows), __builtin_amdgcn_readfirstlane(it.row0)};
-}
-
-// kW weight rows by kX rows in two by two waves, for products too small for whole tiles: a ring of four K steps.
-// A step's second half of fragments is read under the products of the first; the barrier between the two ends
-// every wave's reads of the step, whose slot is filled again at once, and the next step's first half is read under
-// the products of the second.
-template <int kW, int kX>
-__device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, DmaRows<kW / 32>& w, DmaRows<kX / 32>& x, int K,
-                                          const ChunkTail& tail, i32x4 (&acc)[kW / 32][kX / 32]) {
-  constexpr int kStages = 4, kNI = kW / 32, kNJ = kX / 32;
-  constexpr uint32_t kStageBytes = (kW + kX) * kRowBytes;
-  constexpr int kDmaStage = kNI + kNJ;
-  const int tid = item_thread(), lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 15, lk = lane >> 4;
-  const uint32_t lane_chunk = (uint32_t)lr * kRowBytes + (((uint32_t)lk ^ swz(lr)) << 4);
-  const uint32_t a_lane = (uint32_t)((wave & 1) * (kW / 2)) * kRowBytes + lane_chunk;
-  const uint32_t b_lane = (uint32_t)(kW + (wave >> 1) * (kX / 2)) * kRowBytes + lane_chunk;
-#pragma unroll
-  for (int i = 0; i < kNI; ++i)
-#pragma unroll
-    for (int j = 0; j < kNJ; ++j) acc[i][j] = i32x4{};
-  const int nk = ChunkTail::steps(K);
-  const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kNI * 1024;
-  const uint32_t lds_x = lds_addr(lds) + kW * kRowBytes + (uint32_t)wave * kNJ * 1024;
-  int loaded = 0;
-  uint32_t st_load = 0, st_use = 0;
-  auto next = [](uint32_t st) { return st == (kStages - 1) * kStageBytes ? 0u : st + kStageBytes; };
-  auto load = [&]() {
-    static_for<kNI>([&](auto q) {
-      dma16<decltype(q)::value * 1024>(w.base, w.off[decltype(q)::value], lds_w + st_load);
-    });
-    static_for<kNJ>([&](auto q) {
-      dma16<decltype(q)::value * 1024>(x.base, x.off[decltype(q)::value], lds_x + st_load);
-    });
-    advance_to(w, x, ++loaded, nk, tail);
-    st_load = next(st_load);
-  };
-  i32x4 fa[2][kNI], fb[2][kNJ];
-  auto read = [&](int kk) {
-#pragma unroll
-    for (int j = 0; j < kNJ; ++j) fb[kk][j] = *(const i32x4*)(lds + ((b_lane ^ ((uint32_t)kk << 6)) + st_use + j * 16 * kRowBytes));
-#pragma unroll
-    for (int i = 0; i < kNI; ++i) fa[kk][i] = *(const i32x4*)(lds + ((a_lane ^ ((uint32_t)kk << 6)) + st_use + i * 16 * kRowBytes));
-  };
-  auto multiply = [&](int kk) {
-#pragma unroll
-    for (int i = 0; i < kNI; ++i)
-#pragma unroll
-      for (int j = 0; j < kNJ; ++j) I8Mma::mma(acc[i][j], fa[kk][i], fb[kk][j]);
-  };
-  // ahead: K steps behind the next one that may still be in flight; -1: there is no next step.
-  auto step = [&](auto ahead, auto fetch) {
-    constexpr int n = decltype(ahead)::value;
-    read(1);
-    if constexpr (n < 0) {
-      mask_chunks(tail, 0, lk, fa[0]);
-      mask_chunks(tail, 1, lk, fa[1]);
-    }
-    multiply(0);
-    if constexpr (n >= 0) {
-      wait_vm_and_barrier<n * kDmaStage>();
-      st_use = next(st_use);
-      if constexpr (decltype(fetch)::value) load();
-      read(0);
-    }
-    multiply(1);
-  };
-  using std::false_type;
-  advance_to(w, x, 0, nk, tail);
-  for (int ks = 0; ks < min(nk, kStages); ++ks) load();
-  if (nk >= 4)
-    wait_vm_and_barrier<3 * kDmaStage>();
-  else if (nk == 3)
-    wait_vm_and_barrier<2 * kDmaStage>();
-  else if (nk == 2)
-    wait_vm_and_barrier<kDmaStage>();
-  else
-    wait_vm_and_barrier<0>();
-  read(0);
-  for (int ks = 0; ks + kStages < nk; ++ks) step(std::integral_constant<int, 2>{}, std::true_type{});
-  if (nk >= 4) step(std::integral_constant<int, 2>{}, false_type{});
-  if (nk >= 3) step(std::integral_constant<int, 1>{}, false_type{});
-  if (nk >= 2) step(std::integral_constant<int, 0>{}, false_type{});
-  step(std::integral_constant<int, -1>{}, false_type{});
-  mfma_drain(acc);
-  wait_vm_and_barrier<0>();
-}
 
 // One tile of kW weight rows by kX rows, of which it.rows are valid.
 template <bool gated, int kW, int kX>
@@ -367,7 +111,7 @@ __device__ __forceinline__ void small_item(const Q8Args& a, const Item& it, uint
 
   i32x4 acc[kNI][kNJ];
   const ChunkTail tail(K);
-  small_mma<kW, kX>(lds, w, x, K, tail, acc);
+  small_mma<I8Mma, kW, kX>(lds, w, x, K, tail, acc);
 
   float* scales = (float*)(lds + S::kScales);
   if (tid < kW) scales[tid] = my_ws;
@@ -417,18 +161,7 @@ __global__ __launch_bounds__(kThreads, kW + kX <= 128 ? 2 : 1) void q8_small_ker
 
 // ------------------------------------------------------------------------------------ whole tiles
 
-// An accumulator's word.  As assembly: left to itself the compiler copies whole accumulators to vector registers
-// ahead of their use, and spills.
-__device__ __forceinline__ int acc_read(int v) {
-  int r;
-  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(v));
-  return r;
-}
-
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-
-// DMA instructions per wave and K step that a tile's rows take: it computes 32, 64, 128, 192 or 256 of them.
-__device__ __forceinline__ int row_dmas(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : rows <= 192 ? 6 : 8; }
 
 // What a tile's DMAs read.
 template <bool gated>
@@ -628,25 +361,6 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(Q8Args a, int cols
 
 // ------------------------------------------------------------------------------------ few rows
 
-// Row tile t of the experts' rows cut into runs of kTile.
-template <int kTile>
-__device__ __forceinline__ Item find_rows(const Q8Args& a, uint32_t t) {
-  if (!a.offsets) return Item{0, 0, min(kTile, (int)a.rows - (int)t * kTile), (int)t * kTile};
-  Before b;
-  for (int e0 = 0; e0 < a.experts; e0 += 64) {
-    const Experts<kTile> x(a, e0, b);
-    const uint64_t past = __ballot(t < x.end);
-    if (past != 0) {
-      const int l = __builtin_ctzll(past);
-      const uint32_t first = l == 0 ? b.tiles : (uint32_t)__builtin_amdgcn_readlane((int)x.end, l - 1);
-      const int row0 = __builtin_amdgcn_readlane(x.lo, l) + (int)(t - first) * kTile;
-      return Item{e0 + l, 0, min(kTile, __builtin_amdgcn_readlane(x.hi, l) - row0), row0};
-    }
-    b = x.after(a, e0);
-  }
-  return Item{0, 0, 0, 0};
-}
-
 // A tile of 16 kR rows by 16 kN features (gated: kN of each matrix): the four waves take every fourth 128 bytes
 // of K each, straight from memory into registers, so nothing in the loop waits for another wave, and add their
 // sums up in LDS at the end.
@@ -773,19 +487,8 @@ __global__ __launch_bounds__(kThreads) void q8_slim_kernel(Q8Args a) {
   }
 }
 
-// Tiles of `height` rows there can be: every expert may end in a partly filled one.
-int64_t most_tiles(int64_t rows, bool grouped, int32_t experts, int height) {
-  return (rows + height - 1) / height + (grouped ? std::min<int64_t>(experts, rows) : 0);
-}
-
-constexpr int64_t kSlimTiles = 65535;  // they are the grid's second axis
-
 // Workgroups along the features of a slim kernel of 16 `n` features (gated: of each matrix).
 int64_t slim_cols(int32_t N, int n) { return ((int64_t)N + 16 * n - 1) / (16 * n); }
-
-int64_t dealt(int64_t tiles, int cols) {
-  return (tiles * cols + kXcds * kDeal - 1) / (kXcds * kDeal) * (kXcds * kDeal);
-}
 
 template <bool gated, int kN>
 hipError_t launch_slim(const Q8Args& a, hipStream_t s) {

@@ -81,4 +81,21 @@ __device__ __forceinline__ T wave_reduce(T v, F&& f) {
   return v;
 }
 
+// silu(g) * u = (g / (1 + e^-g)) u, from a quarter of g, with the hardware's exponential and reciprocal, each within
+// one fp32 ulp.  The exponent t = -g log2(e) is rounded, which would cost e^-g an error of |g| 2^-24; the rounding r is
+// made good in the first order (e^-g (1 + r ln 2)), as a bf16 result that falls the other way may change the row's
+// 8-bit scale after it.  With a quarter of 1 + e^-g, too, the reciprocal is never a subnormal, which the hardware
+// would flush: it is 2^-126 or more, and 0 from t = 128 on, where e^-g is infinite in fp32.  Where t itself overflows
+// r is infinite; its factor is kept near a quarter.  u comes last, as g u may overflow where silu(g) u does not.
+constexpr float kGateShare = 0.25f;
+__device__ __forceinline__ float sigmoid4(float quarter_g) {  // 4 / (1 + e^-g)
+  constexpr float kLog2e = 4 * 1.44269504f, kLog2eRest = 4 * 1.92596303e-8f, kLn2 = 0.693147181f;
+  constexpr float kLow = 0.15915494f, kHigh = 0.5f;  // constants that an instruction holds
+  const float t = -quarter_g * kLog2e;
+  const float r = fmaf(-quarter_g, kLog2eRest, fmaf(-quarter_g, kLog2e, -t));
+  const float factor = __builtin_amdgcn_fmed3f(fmaf(r, kLn2 / 4, 0.25f), kLow, kHigh);
+  return __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), factor, 0.25f));
+}
+__device__ __forceinline__ float silu_mul(float quarter_g, float u) { return quarter_g * sigmoid4(quarter_g) * u; }
+
 }  // namespace moe
