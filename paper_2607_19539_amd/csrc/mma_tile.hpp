@@ -675,15 +675,15 @@ __device__ __forceinline__ void narrow_mma(uint8_t* __restrict__ lds, DmaRows<kD
 }
 
 // ---------------------------------------------------------------------------
-// kW weight rows by kX rows in two by two waves, for products too small for whole tiles: a ring of four K steps.
+// kW weight rows by kX rows in two by two waves, for products too small for whole tiles: a ring of kStages K steps.
 // A step's second half of fragments is read under the products of the first; the barrier between the two ends
 // every wave's reads of the step, whose slot is filled again at once, and the next step's first half is read under
 // the products of the second.
-template <class Op, int kW, int kX, class LayoutW = ByRow, class LayoutX = ByRow, class W, class Tail>
+template <class Op, int kW, int kX, int kStages = 4, class LayoutW = ByRow, class LayoutX = ByRow, class W, class Tail>
 __device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, W& w, DmaRows<kX / 32>& x, int K, const Tail& tail,
                                           typename Op::Acc (&acc)[kW / 32][kX / 32]) {
   typedef typename Op::Frag Frag;
-  constexpr int kStages = 4, kNI = kW / 32, kNJ = kX / 32;
+  constexpr int kNI = kW / 32, kNJ = kX / 32;
   constexpr uint32_t kStageBytes = (kW + kX) * kRowBytes;
   constexpr int kDmaStage = kNI + kNJ;
   const int tid = item_thread(), lane = tid & 63;
@@ -743,19 +743,17 @@ __device__ __forceinline__ void small_mma(uint8_t* __restrict__ lds, W& w, DmaRo
   using std::false_type;
   advance_to(w, x, 0, nk, tail);
   for (int ks = 0; ks < min(nk, kStages); ++ks) load();
-  if (nk >= 4)
-    wait_vm_and_barrier<3 * kDmaStage>();
-  else if (nk == 3)
-    wait_vm_and_barrier<2 * kDmaStage>();
-  else if (nk == 2)
-    wait_vm_and_barrier<kDmaStage>();
-  else
-    wait_vm_and_barrier<0>();
+  // Step 0 visible, the steps after it in flight.
+  static_for<kStages>([&](auto r) {
+    constexpr int n = kStages - decltype(r)::value;  // steps that are on their way
+    if (n == kStages ? nk >= n : nk == n) wait_vm_and_barrier<(n - 1) * kDmaStage>();
+  });
   read(0);
-  for (int ks = 0; ks + kStages < nk; ++ks) step(std::integral_constant<int, 2>{}, std::true_type{});
-  if (nk >= 4) step(std::integral_constant<int, 2>{}, false_type{});
-  if (nk >= 3) step(std::integral_constant<int, 1>{}, false_type{});
-  if (nk >= 2) step(std::integral_constant<int, 0>{}, false_type{});
+  for (int ks = 0; ks + kStages < nk; ++ks) step(std::integral_constant<int, kStages - 2>{}, std::true_type{});
+  static_for<kStages - 1>([&](auto r) {
+    constexpr int n = kStages - decltype(r)::value;  // steps that are left
+    if (nk >= n) step(std::integral_constant<int, n - 2>{}, false_type{});
+  });
   step(std::integral_constant<int, -1>{}, false_type{});
   mfma_drain(acc);
   wait_vm_and_barrier<0>();

@@ -121,17 +121,19 @@ struct CombineBackwardArgs {
   int32_t k, H;
 };
 
-// Up to kTableTensors tensors as a kernel's argument.  Their elements are taken in chunks, numbered through.
-constexpr int kTableTensors = 128;
+// Up to kMost tensors as a kernel's argument.  Their elements are taken in chunks, numbered through.  A short list has
+// a table of its own: the runtime copies a kernel's arguments at each launch.
+constexpr int kTableTensors = 128, kShortTable = 32;
+template <int kMost>
 struct TensorTable {
-  uint64_t in[kTableTensors];     // address; the top bit marks bf16 (fp32 otherwise)
-  uint64_t out[kTableTensors];
-  int64_t count[kTableTensors];   // elements, none of them 0
-  uint32_t first[kTableTensors];  // the tensor's first chunk
-  uint32_t chunk, chunks;         // elements of a chunk, a multiple of 8; chunks there are
+  uint64_t in[kMost];     // address; the top bit marks bf16 (fp32 otherwise)
+  uint64_t out[kMost];
+  int64_t count[kMost];   // elements, none of them 0
+  uint32_t first[kMost];  // the tensor's first chunk
+  uint32_t chunk, chunks;  // elements of a chunk, a multiple of 8; chunks there are
   int32_t n;
 };
-static_assert(sizeof(TensorTable) <= 3840, "a kernel's arguments have 4 KiB");
+static_assert(sizeof(TensorTable<kTableTensors>) <= 3840, "a kernel's arguments have 4 KiB");
 
 // A launch has fewer than 2^32 threads; one that would need more is refused with hipErrorInvalidConfiguration.
 constexpr bool launch_fits(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
@@ -168,9 +170,11 @@ hipError_t launch_product_dw_plan(const DwPlan& plan, const ProductDwArgs& a, hi
 hipError_t launch_gate(const GateArgs& a, hipStream_t s);
 hipError_t launch_gate_backward(const GateArgs& a, hipStream_t s);
 // parts: a sum of each of the `blocks` workgroups.
-hipError_t launch_squares(const TensorTable& t, double* parts, int blocks, hipStream_t s);
+template <int kMost>
+hipError_t launch_squares(const TensorTable<kMost>& t, double* parts, int blocks, hipStream_t s);
 hipError_t launch_squares_sum(const double* parts, int n, double* total, hipStream_t s);
-hipError_t launch_clip(const TensorTable& t, const double* total, float max_norm, float* norm, int blocks, hipStream_t s);
+template <int kMost>
+hipError_t launch_clip(const TensorTable<kMost>& t, const double* total, float max_norm, float* norm, int blocks, hipStream_t s);
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s);
 
 }  // namespace moe

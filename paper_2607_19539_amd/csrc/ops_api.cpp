@@ -169,16 +169,16 @@ bool overlapping(const moe_tensor_t* t, int32_t n) {
   return false;
 }
 
-// The tables of a list, one after another, to f(table, workgroups).  A workgroup takes a chunk at a time; a list that
-// is large has some 2048 of them, eight to a compute unit, at most as many workgroups.
-constexpr int kListBlocks = 2048;
-template <class F>
+// The tables of a list, one after another, to f(table, workgroups).  Workgroups take a chunk at a time; a long list has
+// some 32 chunks for each.
+constexpr int kListBlocks = 2048;  // eight to a compute unit
+template <int kMost, class F>
 hipError_t for_tables(const moe_tensor_t* t, int32_t n, F&& f) {
   int64_t all = 0;
   for (int32_t i = 0; i < n; ++i) all += t[i].count;
   // At least 4096 elements, and few enough chunks for their number.
-  const int64_t chunk = std::min<int64_t>(std::max<int64_t>((all / kListBlocks + 4095) / 4096 * 4096, 4096), 1 << 30);
-  TensorTable table;
+  const int64_t chunk = std::min<int64_t>((all / (32 * kListBlocks) / 4096 + 1) * 4096, 1 << 30);
+  TensorTable<kMost> table;
   table.n = 0;
   table.chunks = 0;
   table.chunk = (uint32_t)chunk;
@@ -190,7 +190,7 @@ hipError_t for_tables(const moe_tensor_t* t, int32_t n, F&& f) {
   };
   for (int32_t i = 0; i < n; ++i) {
     if (t[i].count == 0) continue;
-    if (table.n == kTableTensors)
+    if (table.n == kMost)
       if (hipError_t e = flush()) return e;
     table.in[table.n] = (uint64_t)t[i].data | (t[i].type == MOE_TYPE_BF16 ? 1ull << 63 : 0);
     table.out[table.n] = (uint64_t)t[i].out;
@@ -199,6 +199,10 @@ hipError_t for_tables(const moe_tensor_t* t, int32_t n, F&& f) {
     table.chunks += (uint32_t)((t[i].count + chunk - 1) / chunk);
   }
   return table.n ? flush() : hipSuccess;
+}
+template <class F>
+hipError_t for_each_table(const moe_tensor_t* t, int32_t n, F&& f) {
+  return n <= kShortTable ? for_tables<kShortTable>(t, n, f) : for_tables<kTableTensors>(t, n, f);
 }
 
 }  // namespace
@@ -498,7 +502,7 @@ int moe_squares(const moe_tensor_t* tensors, int32_t n, double* total, void* wor
     return record_error(MOE_ECAPACITY, who, "the workspace is smaller than moe_squares_workspace says");
   const hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  hipError_t e = for_tables(tensors, n, [&](const TensorTable& t, int blocks) {
+  hipError_t e = for_each_table(tensors, n, [&](const auto& t, int blocks) {
     const hipError_t one = launch_squares(t, (double*)workspace + parts, blocks, s);
     parts += blocks;
     return one;
@@ -520,13 +524,13 @@ int moe_clip(const moe_tensor_t* tensors, int32_t n, const double* total, float 
   }
   const hipStream_t s = (hipStream_t)stream;
   bool told = false;
-  hipError_t e = for_tables(tensors, n, [&](const TensorTable& t, int blocks) {
+  hipError_t e = for_each_table(tensors, n, [&](const auto& t, int blocks) {
     const hipError_t one = launch_clip(t, total, max_norm, told ? nullptr : norm, blocks, s);
     told = true;
     return one;
   });
   if (e == hipSuccess && !told && norm) {  // no tensors: the norm alone
-    TensorTable none;
+    TensorTable<kShortTable> none;
     none.n = 0;
     none.chunks = 0;
     none.chunk = 4096;

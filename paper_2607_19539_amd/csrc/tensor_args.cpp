@@ -28,13 +28,11 @@ bool of_kind(at::ScalarType t, long kind) {
 // Kinds from here on: the tensor is on the current device, too.
 constexpr long kHere = 16;
 
-bool here(const at::Tensor& t) {
-  return t.is_cuda() && t.device().index() == c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
-}
+c10::DeviceIndex current_device() { return c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index(); }
 
 bool fits(const at::Tensor& t, PyObject* shape, long kind) {
   if (kind >= kHere) {
-    if (!here(t)) return false;
+    if (!t.is_cuda() || t.device().index() != current_device()) return false;
     kind -= kHere;
   }
   if (!of_kind(t.scalar_type(), kind) || !PyTuple_Check(shape)) return false;
@@ -98,6 +96,7 @@ PyObject* table(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const Py_ssize_t m = PySequence_Fast_GET_SIZE(tensors);
   PyObject* bytes = nullptr;
   bool good = !outs || PySequence_Fast_GET_SIZE(outs) == m;
+  c10::DeviceIndex device = -1;  // asked for at the first tensor that is on a device
   try {
     bytes = PyBytes_FromStringAndSize(nullptr, m * (Py_ssize_t)sizeof(Entry));
     Entry* e = bytes ? (Entry*)PyBytes_AS_STRING(bytes) : nullptr;
@@ -107,8 +106,10 @@ PyObject* table(PyObject*, PyObject* const* args, Py_ssize_t n) {
       good = THPVariable_Check(p) && THPVariable_Check(q);
       if (!good) break;
       const at::Tensor &t = THPVariable_Unpack(p), &o = THPVariable_Unpack(q);
-      good = of_kind(t.scalar_type(), 5) && o.scalar_type() == t.scalar_type() && o.numel() == t.numel() && here(t) && here(o) &&
-             t.is_contiguous() && o.is_contiguous();
+      good = of_kind(t.scalar_type(), 5) && o.scalar_type() == t.scalar_type() && o.numel() == t.numel() && t.is_cuda() &&
+             o.is_cuda() && t.is_contiguous() && o.is_contiguous();
+      if (good && device < 0) device = current_device();
+      good = good && t.device().index() == device && o.device().index() == device;
       if (good) e[i] = Entry{t.data_ptr(), o.data_ptr(), t.numel(), t.scalar_type() == at::kBFloat16, 0};
     }
   } catch (const std::exception& x) {
