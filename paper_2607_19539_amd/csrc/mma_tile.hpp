@@ -240,6 +240,16 @@ struct Bf16Mma {
   }
 };
 
+// The same product left to the compiler, for kernels that the weights' reading bounds: it may move accumulators, and keeps
+// the distances itself.
+struct Bf16MmaBuiltin {
+  typedef bf16x8 Frag;
+  typedef f32x4 Acc;
+  static __device__ __forceinline__ void mma(Acc& d, const Frag& a, const Frag& b) {
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
+  }
+};
+
 // The same shape in bytes with twice the products: 64 k of int8, summed in 32-bit integers.
 struct I8Mma {
   typedef i32x4 Frag;
@@ -331,6 +341,14 @@ __device__ __forceinline__ void mask_elements(const Tail& tail, int kk, int lk, 
     }
   }
 }
+
+// An operand's source one K step back, at the last of its tile.
+template <int kDma>
+__device__ __forceinline__ void step_back(DmaRows<kDma>& r) {
+  r.base -= r.step;
+}
+template <int kDma>
+__device__ __forceinline__ void step_back(IndexedRows<kDma>&) {}  // it does not leave its rows
 
 // An operand's source at K step `next`, one step on from where it was.
 template <int kDma>
@@ -546,6 +564,135 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRow
   // All waves are done reading LDS before the epilogue or the next tile reuses it.
   wait_vm_and_barrier<0>();
 }
+
+// ---------------------------------------------------------------------------
+// The same K step for tiles that follow one another without a pause: the last two steps of a tile fetch the first two of
+// the next, and its last quarter reads the next one's first fragments, so that the ring never runs dry and the next
+// tile's products start right after the epilogue.  (With tile_start under the epilogue the ring is filled anew for each
+// tile, by all compute units at once.)
+//   begin   after tile_start: the first fragments
+//   run     the K loop.  early(): before the first step.  late(): two K steps before the end (or one); w and x then are
+//           at the next tile's first step, and next(k) moves them to its step k.  Where no tile of this height follows,
+//           they stay at a step of this one (fetched for nothing: a question at each DMA costs more), and end() waits
+//           for what is on its way.
+// K has two steps or more where a tile follows, and so has that one.
+// ---------------------------------------------------------------------------
+template <class Op, class LayoutW, class LayoutX, int kNJ>
+struct TileStream {
+  typedef typename Op::Frag Frag;
+  static_assert(kNJ == 4 || kNJ == 6 || kNJ == 8, "token fragments per wave");
+  static_assert(!LayoutX::transposed || kNJ != 6, "a wave's tokens start on half a panel or on a panel");
+  static constexpr int kHJ = kNJ / 2;
+  uint8_t* lds;
+  uint32_t o0, o1, o2, o3, o4;  // ring slots: this step's weights and tokens, the next one's, the free one
+  Frag fa[8], fb[kNJ];
+
+  __device__ __forceinline__ void begin(uint8_t* lds_, int nk) {
+    lds = lds_;
+    o0 = 0, o1 = kBlockBytes, o2 = 2 * kBlockBytes, o3 = 3 * kBlockBytes, o4 = 4 * kBlockBytes;
+    if (nk > 1)
+      wait_vm_and_barrier<kDmaPerThread + kNJ>();
+    else
+      wait_vm_and_barrier<0>();
+    const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+    const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * 128), lane);
+    const Fragments<LayoutX, Frag> b_lane((uint32_t)((wave >> 1) * 16 * kNJ), lane);
+#pragma unroll
+    for (int j = 0; j < kHJ; ++j) fb[j] = b_lane.read(lds, o1, 0, j * 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fa[i] = a_lane.read(lds, o0, 0, i * 16);
+  }
+
+  template <class W, class X, class Tail, class Early, class Late, class Next>
+  __device__ __forceinline__ void run(W& w, X& x, int nk, const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Early&& early, Late&& late,
+                                      Next&& next) {
+    const int tid = item_thread(), lane = tid & 63, lk = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * 128), lane);
+    const Fragments<LayoutX, Frag> b_lane((uint32_t)((wave >> 1) * 16 * kNJ), lane);
+    const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
+    const uint32_t lds_x = lds_addr(lds) + (uint32_t)wave * kNJ * 1024;
+    auto read_a = [&](uint32_t slot, int kk, int i) { fa[i] = a_lane.read(lds, slot, kk, i * 16); };
+    auto read_b = [&](uint32_t slot, int kk, int j) { fb[j] = b_lane.read(lds, slot, kk, j * 16); };
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < kNJ; ++j) acc[i][j] = typename Op::Acc{};
+    // Halves and DMAs as in tile_run.
+    auto w_dma = [](int quarter, int i) { return quarter < 2 && i % 2 == 0 ? quarter * 4 + i / 2 : -1; };
+    auto half0 = [&](auto kkc, auto dma) {
+      constexpr int kk = decltype(kkc)::value;
+      static_for<8 * kHJ>([&](auto p) {
+        constexpr int i = decltype(p)::value / kHJ, j = decltype(p)::value % kHJ;
+        constexpr int js = i & 1 ? kHJ - 1 - j : j;
+        constexpr int wq = decltype(dma)::value && j == kHJ / 2 ? w_dma(2 * kk, i) : -1;
+        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o4);
+        Op::mma(acc[i][js], fa[i], fb[js]);
+        if constexpr (wq >= 0) dma16_at_m0(w.base, w.off[wq]);
+        if constexpr (j == 1 && i < kHJ) read_b(o1, kk, kHJ + i);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto half1 = [&](uint32_t sa, uint32_t sb, auto kk1c) {
+      constexpr int kk1 = decltype(kk1c)::value;
+      static_for<8 * kHJ>([&](auto p) {
+        constexpr int i = decltype(p)::value / kHJ, j = decltype(p)::value % kHJ;
+        constexpr int js = kHJ + (i & 1 ? kHJ - 1 - j : j);
+        constexpr bool fetch_x = kk1 == 0 && j == kHJ / 2 && i < kNJ;
+        constexpr int wq = kk1 == 1 && j == kHJ / 2 ? w_dma(1, i) : -1;
+        if constexpr (fetch_x) dma_m0<i * 1024>(lds_x + o0);
+        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o4);
+        Op::mma(acc[i][js], fa[i], fb[js]);
+        if constexpr (fetch_x) dma16_at_m0(x.base, x.off[i]);
+        if constexpr (wq >= 0) dma16_at_m0(w.base, w.off[wq]);
+        if constexpr (j == 0 && i < kHJ) read_b(sb, kk1, i);
+        if constexpr (j == kHJ - 1) read_a(sa, kk1, i);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    // last: elements past K's end are zeroed.
+    auto step = [&](auto last) {
+      constexpr bool kLast = decltype(last)::value;
+      using first = std::integral_constant<int, 0>;
+      using second = std::integral_constant<int, 1>;
+      auto mask0 = [&](int kk) {
+        if constexpr (kLast) {
+          mask_elements(tail, kk, lk, fa, 0, 8);
+          mask_elements(tail, kk, lk, fb, 0, kHJ);
+        }
+      };
+      auto mask1 = [&](int kk) {
+        if constexpr (kLast) mask_elements(tail, kk, lk, fb, kHJ, kHJ);
+      };
+      mask0(0);
+      half0(first{}, std::true_type{});
+      mask1(0);
+      half1(o0, o1, second{});
+      mask0(1);
+      half0(second{}, std::false_type{});
+      mask1(1);
+      wait_vm_and_barrier<kDmaPerThread>();  // the next step visible, this one's slots free
+      half1(o2, o3, first{});
+      const uint32_t t0 = o0, t1 = o1;
+      o0 = o2, o1 = o3, o2 = o4, o3 = t0, o4 = t1;
+    };
+    early();
+    for (int ks = 0; ks + 2 < nk; ++ks) {
+      step(std::false_type{});
+      advance_to(w, x, ks + 3, nk, tail);
+    }
+    late();
+    if (nk > 1) {
+      step(std::false_type{});
+      next(1);
+    }
+    step(std::true_type{});
+    next(2);
+    mfma_drain(acc);
+  }
+  // All waves are done reading LDS before what comes next writes it.
+  __device__ __forceinline__ void end() const { wait_vm_and_barrier<0>(); }
+};
 
 template <class Op, int kNJ, class Tail, class Late>
 __device__ __forceinline__ void tile_mma(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,

@@ -156,6 +156,7 @@ template <bool by_k>
 struct ProductSource {
   DmaRows<kDmaPerThread> w;
   DmaRows<8> x;
+  uint32_t row[8];  // of x, for the tile whose addresses come next
   // First the rows, which may have to be looked up ...
   __device__ __forceinline__ void rows(const ProductArgs& a, const Item& it) {
     const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
@@ -163,7 +164,7 @@ struct ProductSource {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int n = (wave * dx + i) * kRowsPerDma + (lane >> 3), m = it.row0 + min(n, it.rows - 1);
-      x.off[i] = (uint32_t)(a.index ? a.index[m] : m);
+      row[i] = (uint32_t)(a.index ? a.index[m] : m);
     }
   }
   // ... then the addresses.
@@ -177,15 +178,15 @@ struct ProductSource {
     x.base = a.x_rows > 0 ? (const uint8_t*)(a.x + (int64_t)row0 * K) : (const uint8_t*)a.w;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t r = x.off[i], n = (uint32_t)((wave * dx + i) * kRowsPerDma) + ((uint32_t)lane >> 3);
+      const uint32_t n = (uint32_t)((wave * dx + i) * kRowsPerDma) + ((uint32_t)lane >> 3);
       const uint32_t c = min(((uint32_t)lane & 7) ^ swz(n), cmax);
-      x.off[i] = (named(a, r) ? (r - (uint32_t)row0) * (uint32_t)K * 2 : 0u) + (c << 4);
+      x.off[i] = (named(a, row[i]) ? (row[i] - (uint32_t)row0) * (uint32_t)K * 2 : 0u) + (c << 4);
       asm volatile("" ::"v"(x.off[i]));  // complete before the first DMA, which the compiler does not count
     }
   }
   template <int kDma>
   __device__ __forceinline__ DmaRows<kDma> first_rows() const {
-    DmaRows<kDma> r{x.base, x.step, {}};
+    DmaRows<kDma> r{x.base, kRowBytes, {}};
 #pragma unroll
     for (int i = 0; i < kDma; ++i) r.off[i] = x.off[i];
     return r;
@@ -214,73 +215,140 @@ struct ProductSource {
   }
 };
 
-// The K loop and the epilogue of a tile of 32 kDma rows by 256 features, whose first K steps `src` has started.
-// Between the two the next item's are started, so that they arrive under the epilogue, which keeps to registers.
-template <bool by_k, int kDma>
-__device__ __forceinline__ void tile_item(const ProductArgs& a, const Item& it, const Item& next, ProductSource<by_k>& src, uint8_t* lds) {
-  constexpr bool kNarrow = kDma <= 2;             // four waves by the features alone
-  constexpr int kNI = kNarrow ? 4 : 8;            // weight fragments per wave
-  constexpr int kNJ = kNarrow ? 2 * kDma : kDma;  // row fragments per wave
-  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
-  const int N = a.N;
-  auto quad_n = [&](int i) {
-    return kNarrow ? (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16 : (wave & 1) * 128 + i * 16;
-  };
-  auto quad_m = [&](int j, int lane) { return (kNarrow ? 0 : (wave >> 1) * (16 * kNJ)) + j * 16 + (lane & 15); };
-  const int first = it.col * 256;
-  DmaRows<kDma> x = src.template first_rows<kDma>();
-  f32x4 acc[kNI][kNJ];
-  const ElementTail tail = tail_of<by_k>(a);
-  // Which rows there are, and the next item's, are asked for near the loop's end: all are there when it ends, and no
-  // wait for them meets a DMA.
-  uint32_t r[kNJ];
-  auto late = [&] {
-    const int lane = item_thread() & 63;
+// The finished tile: acc[i][j] holds features quad_n(i) + 4 lk on of row quad_m(j) + lr, r[j] that row's of x.
+// A lane has 4 consecutive features of a row in each of two fragments; the lanes 16 apart exchange quads, so that
+// each stores 8 consecutive features of one.  A tall tile that is full, of rows that are there, is stored without a question.
+template <bool tall, int kNI, int kNJ, class QuadN, class QuadM>
+__device__ __forceinline__ void store_tile(const ProductArgs& a, const Item& it, f32x4 (&acc)[kNI][kNJ], const uint32_t (&r)[kNJ],
+                                           QuadN&& quad_n, QuadM&& quad_m) {
+  const int lane = item_thread() & 63, lk = lane >> 4, N = a.N, first = it.col * 256;
+  auto store = [&](auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll
     for (int j = 0; j < kNJ; ++j) {
-      const int m = it.row0 + min(quad_m(j, lane), it.rows - 1);
-      r[j] = (uint32_t)(a.index ? a.index[m] : m);
+      const bool ok = named(a, r[j]);
+      const int m = quad_m(j, lane), f = first + (lk & 1) * 16 + (lk >> 1) * 8;
+      uint16_t* row = a.out + (int64_t)(it.row0 + m) * N + f;
+#pragma unroll
+      for (int i = 0; i < kNI; i += 2) {
+        uint32_t h[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float v[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v[q] = acc_read(acc[i + u][j][q]);
+            if (!kWhole && !ok) v[q] = kNan;
+          }
+          h[u][0] = bf16x2_of(v[0], v[1]);
+          h[u][1] = bf16x2_of(v[2], v[3]);
+        }
+        const auto lo = __builtin_amdgcn_permlane16_swap(h[0][0], h[1][0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(h[0][1], h[1][1], false, false);
+        if (kWhole || (m < it.rows && f + quad_n(i) < N)) *(u32x4*)(row + quad_n(i)) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+        __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
+      }
     }
+  };
+  if constexpr (tall) {
+    bool all = it.rows == 32 * kNJ && first + 256 <= N;
+#pragma unroll
+    for (int j = 0; j < kNJ; ++j) all = all && named(a, r[j]);
+    if (__all(all)) return store(std::true_type{});
+  }
+  store(std::false_type{});
+}
+
+// Which rows of x a lane's columns of a tile are.
+template <int kNJ, class QuadM>
+__device__ __forceinline__ void lane_rows(const ProductArgs& a, const Item& it, uint32_t (&r)[kNJ], QuadM&& quad_m) {
+  const int lane = item_thread() & 63;
+#pragma unroll
+  for (int j = 0; j < kNJ; ++j) {
+    const int m = it.row0 + min(quad_m(j, lane), it.rows - 1);
+    r[j] = (uint32_t)(a.index ? a.index[m] : m);
+  }
+}
+template <int n>
+__device__ __forceinline__ void arrived(const uint32_t (&r)[n]) {  // the compiler waits for them here, not under later DMAs
+#pragma unroll
+  for (int j = 0; j < n; ++j) asm volatile("" ::"v"(r[j]));
+}
+
+// Tiles of up to 64 rows, whose first K steps `src` has started: the K loop, the next item's start, which find() gives,
+// and under it the epilogue.  Leaves the next item in `it`.
+template <bool by_k, int kDma, class Find>
+__device__ __forceinline__ void narrow_item(const ProductArgs& a, Item& it, ProductSource<by_k>& src, uint8_t* lds, Find&& find) {
+  constexpr int kNJ = 2 * kDma;
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  auto quad_n = [&](int i) { return (wave >> 1) * 128 + (i >> 1) * 64 + (wave & 1) * 32 + (i & 1) * 16; };
+  auto quad_m = [&](int j, int lane) { return j * 16 + (lane & 15); };
+  DmaRows<kDma> x = src.template first_rows<kDma>();
+  f32x4 acc[4][kNJ];
+  uint32_t r[kNJ];
+  const Item next = find();
+  // Which rows there are, and the next item's, are asked for near the loop's end: all are there when it ends.
+  auto late = [&] {
+    lane_rows(a, it, r, quad_m);
     if (next.rows > 0) src.rows(a, next);
   };
-  if constexpr (kNarrow)
-    narrow_run<Bf16Mma, WeightLayout<by_k>>(lds, src.w, x, a.K, tail, acc, late, [] {});
-  else
-    tile_run<Bf16Mma, WeightLayout<by_k>>(lds, src.w, x, a.K, tail, acc, late, [] {});
-#pragma unroll
-  for (int j = 0; j < kNJ; ++j) asm volatile("" ::"v"(r[j]));
+  narrow_run<Bf16MmaBuiltin, WeightLayout<by_k>>(lds, src.w, x, a.K, tail_of<by_k>(a), acc, late, [] {});
+  arrived(r);
   if (next.rows > 0) {
     src.addresses(a, next);
     src.start(a, next, lds);
   }
-  const int lane = item_thread() & 63, lk = lane >> 4;
-  // A lane has 4 consecutive features of a row in each of two fragments; the lanes 16 apart exchange quads, so that
-  // each stores 8 consecutive features of one.
-#pragma unroll
-  for (int i = 0; i < kNI; i += 2) {
-    const int f = first + quad_n(i) + (lk & 1) * 16 + (lk >> 1) * 8;
-#pragma unroll
-    for (int j = 0; j < kNJ; ++j) {
-      uint32_t h[2][2];
-      const bool ok = named(a, r[j]);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v[q] = acc_read(acc[i + u][j][q]);
-          if (!ok) v[q] = kNan;
-        }
-        h[u][0] = bf16x2_of(v[0], v[1]);
-        h[u][1] = bf16x2_of(v[2], v[3]);
+  store_tile<false>(a, it, acc, r, quad_n, quad_m);
+  it = next;
+}
+
+// Tiles of 32 kDma rows one after another, as long as the next item is as high, the first one started by `src`.  Leaves
+// the next item in `it`, started.
+template <bool by_k, int kDma, class Find>
+__device__ __forceinline__ void tall_items(const ProductArgs& a, Item& it, ProductSource<by_k>& src, uint8_t* lds, Find&& find) {
+  const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
+  auto quad_n = [&](int i) { return (wave & 1) * 128 + i * 16; };
+  auto quad_m = [&](int j, int lane) { return (wave >> 1) * (16 * kDma) + j * 16 + (lane & 15); };
+  const ElementTail tail = tail_of<by_k>(a);
+  const int nk = ElementTail::steps(a.K);
+  DmaRows<kDma> x = src.template first_rows<kDma>();
+  TileStream<Bf16Mma, WeightLayout<by_k>, ByRow, kDma> stream;
+  stream.begin(lds, nk);
+  bool follows;
+  do {
+    f32x4 acc[8][kDma];
+    uint32_t r[kDma];
+    Item next;
+    auto early = [&] {
+      lane_rows(a, it, r, quad_m);
+      next = find();
+      if (next.rows > 0) src.rows(a, next);
+    };
+    auto late = [&] {
+      arrived(r);
+      follows = nk > 1 && next.rows > 0 && row_dmas(next.rows) == kDma;
+      if (follows) {
+        src.addresses(a, next);
+        x = src.template first_rows<kDma>();
+        advance_to(src.w, x, 0, nk, tail);
+      } else {
+        step_back(src.w);
+        step_back(x);
       }
-      const auto lo = __builtin_amdgcn_permlane16_swap(h[0][0], h[1][0], false, false);
-      const auto hi = __builtin_amdgcn_permlane16_swap(h[0][1], h[1][1], false, false);
-      const int m = quad_m(j, lane);
-      if (m < it.rows && f < N) *(u32x4*)(a.out + (int64_t)(it.row0 + m) * N + f) = u32x4{lo[0], hi[0], lo[1], hi[1]};
-      __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
+    };
+    stream.run(src.w, x, nk, tail, acc, early, late, [&](int k) {
+      if (follows) advance_to(src.w, x, k, nk, tail);
+    });
+    if (!follows) {
+      stream.end();
+      if (next.rows > 0) {
+        src.addresses(a, next);
+        src.start(a, next, lds);
+      }
     }
-  }
+    store_tile<true>(a, it, acc, r, quad_n, quad_m);
+    it = next;
+  } while (follows);
 }
 
 // Workgroups that stay: b takes item (b / 8 + 7 n) mod (workgroups of its XCD) of the n-th set that its XCD's
@@ -292,23 +360,25 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
   const Items<256> items(a, cols);
   const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, set = gridDim.x / kXcds;
   uint32_t n = 0;
-  Item it = uniform(items.find(a, xcd, mine));
+  auto find = [&] {
+    const uint32_t j = n * set + (mine + 7 * n) % set;
+    ++n;
+    return uniform(items.find(a, xcd, j));
+  };
+  Item it = find();
   if (it.rows <= 0) return;
   ProductSource<by_k> src;
   src.rows(a, it);
   src.addresses(a, it);
   src.start(a, it, lds);
   while (it.rows > 0) {
-    ++n;
-    const Item next = uniform(items.find(a, xcd, n * set + (mine + 7 * n) % set));
     switch (row_dmas(it.rows)) {
-      case 1: tile_item<by_k, 1>(a, it, next, src, lds); break;
-      case 2: tile_item<by_k, 2>(a, it, next, src, lds); break;
-      case 4: tile_item<by_k, 4>(a, it, next, src, lds); break;
-      case 6: tile_item<by_k, 6>(a, it, next, src, lds); break;
-      default: tile_item<by_k, 8>(a, it, next, src, lds); break;
+      case 1: narrow_item<by_k, 1>(a, it, src, lds, find); break;
+      case 2: narrow_item<by_k, 2>(a, it, src, lds, find); break;
+      case 4: tall_items<by_k, 4>(a, it, src, lds, find); break;
+      case 6: tall_items<by_k, 6>(a, it, src, lds, find); break;
+      default: tall_items<by_k, 8>(a, it, src, lds, find); break;
     }
-    it = next;
   }
 }
 

@@ -133,19 +133,27 @@ __device__ __forceinline__ bool any_bad(const DmaRows<kDma>&) { return false; }
 template <int kDma>
 __device__ __forceinline__ bool any_bad(const IndexedRows<kDma>& d) { return __any(d.bad); }
 
-// Four consecutive k of dw[e, n, :], or of a part of it.
-__device__ __forceinline__ void store4(const ProductDwArgs& a, const DwItem& it, int split, int n, int k, f32x4 v) {
-  if (n >= a.N || k >= a.K) return;
-  const int64_t at = ((int64_t)it.expert * a.N + n) * a.K + k;
+// Element `at` of dw and the three after it, or of a part of it.
+template <bool add>
+__device__ __forceinline__ void store4(const ProductDwArgs& a, const DwItem& it, int split, int64_t at, f32x4 v) {
   if (split > 1) {
     *(f32x4*)(a.parts + (int64_t)it.part * a.experts * a.N * a.K + at) = v;
   } else if (a.bf16) {
     *(u32x2*)((uint16_t*)a.dw + at) = u32x2{bf16x2_of(v[0], v[1]), bf16x2_of(v[2], v[3])};
   } else {
     f32x4* out = (f32x4*)((float*)a.dw + at);
-    if (a.accumulate) v += *out;
+    if constexpr (add) v += *out;
     *out = v;
   }
+}
+// Four consecutive k of dw[e, n, :], if they are inside.
+__device__ __forceinline__ void store_inside(const ProductDwArgs& a, const DwItem& it, int split, int n, int k, f32x4 v) {
+  if (n >= a.N || k >= a.K) return;
+  const int64_t at = ((int64_t)it.expert * a.N + n) * a.K + k;
+  if (a.accumulate)
+    store4<true>(a, it, split, at, v);
+  else
+    store4<false>(a, it, split, at, v);
 }
 
 // ------------------------------------------------------------------------------------ small tiles
@@ -185,7 +193,7 @@ __global__ __launch_bounds__(kThreads, kTile <= 64 ? 4 : 2) void dw_small_kernel
     for (int j = 0; j < kN; ++j) {
       f32x4 v = acc[i][j];
       if (bad) v = f32x4{kNan, kNan, kNan, kNan};
-      store4(a, it, split, it.n0 + (wave >> 1) * (kTile / 2) + j * 16 + lr, it.k0 + (wave & 1) * (kTile / 2) + i * 16 + 4 * lk, v);
+      store_inside(a, it, split, it.n0 + (wave >> 1) * (kTile / 2) + j * 16 + lr, it.k0 + (wave & 1) * (kTile / 2) + i * 16 + 4 * lk, v);
     }
 }
 
@@ -213,11 +221,11 @@ struct DwSource {
   }
 };
 
-// The K loop and the epilogue of a tile of 256 k by 32 kDma n, whose first K steps `src` has started.  The next item's
-// are started between the two.
-template <bool indexed, int kDma>
-__device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, const DwItem& it, const DwItem& next, DwSource<indexed>& src,
-                                             uint8_t* lds) {
+// The K loop and the epilogue of a tile of 256 k by 32 kDma n, whose first K steps `src` has started.  Those of the next
+// item, which find() gives, are started between the two.
+template <bool indexed, int kDma, class Find>
+__device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, const DwItem& it, DwItem& next, DwSource<indexed>& src,
+                                             uint8_t* lds, Find&& find) {
   const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
   f32x4 acc[8][kDma];
   bool bad = false;
@@ -225,9 +233,10 @@ __device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, 
     DmaRows<kDma> y{src.y.base, (uint32_t)kTileK * (uint32_t)a.N * 2, {}};
 #pragma unroll
     for (int i = 0; i < kDma; ++i) y.off[i] = src.y.off[i];
-    tile_run<Bf16Mma, ByK, ByK>(lds, src.x, y, it.rows, tail_of<indexed>(a, it.rows), acc, [] {}, [] {});
+    tile_run<Bf16Mma, ByK, ByK>(lds, src.x, y, it.rows, tail_of<indexed>(a, it.rows), acc, [&] { next = find(); }, [] {});
     bad = any_bad(src.x);  // every wave has met every row
   } else {
+    next = find();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -238,19 +247,33 @@ __device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, 
   }
   if (next.rows > 0) src.start(a, next, lds);
   const int lane = item_thread() & 63, lr = lane & 15, lk = lane >> 4;
+  // A tile that lies within dw, and replaces it, is stored without a question: the others' cost a tile 2 us.
+  auto store = [&](auto plain) {
+    constexpr bool kPlain = decltype(plain)::value;
 #pragma unroll
-  for (int j = 0; j < kDma; ++j)
+    for (int j = 0; j < kDma; ++j) {
+      const int n = it.n0 + (wave >> 1) * (16 * kDma) + j * 16 + lr, k = it.k0 + (wave & 1) * 128 + 4 * lk;
+      const int64_t row = ((int64_t)it.expert * a.N + n) * a.K + k;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f32x4 v;
+      for (int i = 0; i < 8; ++i) {
+        f32x4 v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v[q] = acc_read(acc[i][j][q]);
-        if (bad) v[q] = kNan;
+        for (int q = 0; q < 4; ++q) {
+          v[q] = acc_read(acc[i][j][q]);
+          if (!kPlain && bad) v[q] = kNan;
+        }
+        if constexpr (kPlain)
+          store4<false>(a, it, split, row + i * 16, v);
+        else
+          store_inside(a, it, split, n, k + i * 16, v);
+        __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
       }
-      store4(a, it, split, it.n0 + (wave >> 1) * (16 * kDma) + j * 16 + lr, it.k0 + (wave & 1) * 128 + i * 16 + 4 * lk, v);
-      __builtin_amdgcn_sched_barrier(0);  // block by block, or the accumulators are all read at once
     }
+  };
+  if (!bad && !a.accumulate && it.n0 + 32 * kDma <= a.N && it.k0 + 256 <= a.K)
+    store(std::true_type{});
+  else
+    store(std::false_type{});
 }
 
 // Workgroups that stay, a compute unit each; the 32 of an XCD take runs of consecutive items.
@@ -259,17 +282,21 @@ __global__ __launch_bounds__(kThreads, 1) void dw_tile_kernel(ProductDwArgs a, i
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
   ExpertRows experts(a);
   const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds, set = gridDim.x / kXcds;
-  auto find = [&](uint32_t n) { return uniform(dw_item<256>(a, experts, split, (n * kXcds + xcd) * set + (mine + 7 * n) % set)); };
   uint32_t n = 0;
-  DwItem it = find(0);
+  auto find = [&] {
+    const uint32_t at = (n * kXcds + xcd) * set + (mine + 7 * n) % set;
+    ++n;
+    return uniform(dw_item<256>(a, experts, split, at));
+  };
+  DwItem it = find();
   DwSource<indexed> src;
   if (it.rows > 0) src.start(a, it, lds);
   while (it.expert >= 0) {
-    const DwItem next = find(++n);
+    DwItem next;
     if (a.N - it.n0 > 128)
-      dw_tile_item<indexed, 8>(a, split, it, next, src, lds);
+      dw_tile_item<indexed, 8>(a, split, it, next, src, lds, find);
     else
-      dw_tile_item<indexed, 4>(a, split, it, next, src, lds);
+      dw_tile_item<indexed, 4>(a, split, it, next, src, lds, find);
     it = next;
   }
 }
