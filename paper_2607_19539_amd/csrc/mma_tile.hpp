@@ -342,14 +342,6 @@ __device__ __forceinline__ void mask_elements(const Tail& tail, int kk, int lk, 
   }
 }
 
-// An operand's source one K step back, at the last of its tile.
-template <int kDma>
-__device__ __forceinline__ void step_back(DmaRows<kDma>& r) {
-  r.base -= r.step;
-}
-template <int kDma>
-__device__ __forceinline__ void step_back(IndexedRows<kDma>&) {}  // it does not leave its rows
-
 // An operand's source at K step `next`, one step on from where it was.
 template <int kDma>
 __device__ __forceinline__ void next_step(DmaRows<kDma>& r, int) {
@@ -567,16 +559,32 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRow
 
 // ---------------------------------------------------------------------------
 // The same K step for tiles that follow one another without a pause: the last two steps of a tile fetch the first two of
-// the next, and its last quarter reads the next one's first fragments, so that the ring never runs dry and the next
-// tile's products start right after the epilogue.  (With tile_start under the epilogue the ring is filled anew for each
-// tile, by all compute units at once.)
-//   begin   after tile_start: the first fragments
-//   run     the K loop.  early(): before the first step.  late(): two K steps before the end (or one); w and x then are
-//           at the next tile's first step, and next(k) moves them to its step k.  Where no tile of this height follows,
-//           they stay at a step of this one (fetched for nothing: a question at each DMA costs more), and end() waits
-//           for what is on its way.
+// the next, so that the ring never runs dry and the next tile's products start right after the epilogue.  (With tile_start
+// under the epilogue the ring is filled anew for each tile, by all compute units at once.)
+//   begin   after tile_start: a ring of its own
+//   resume  the ring as the tile before left it, which has fetched the first two steps of this one
+//   run     the K loop.  early(): before the first step.  late(): two K steps before the end (or one); it gives the token
+//           DMAs of the tile that follows, 4, 6 or 8, whose first step w and x then are at, and next(k) moves them to its
+//           step k; or 0 where none does.
+//   end     where none follows
 // K has two steps or more where a tile follows, and so has that one.
 // ---------------------------------------------------------------------------
+struct Ring {
+  uint32_t o0, o1, o2, o3, o4;  // slots: this step's weights and tokens, the next one's, the free one
+};
+
+// The DMA at M0, if n > kAbove.  A branch that the compiler does not see: between its own it would move accumulators.
+template <int kAbove>
+__device__ __forceinline__ void dma16_at_m0_if(uint32_t n, const uint8_t* sbase, uint32_t voff) {
+  asm volatile("s_cmp_gt_u32 %2, %3\n\ts_cbranch_scc0 .Lno_dma%=\n\tglobal_load_lds_dwordx4 %0, %1\n.Lno_dma%=:" ::"v"(voff), "s"(sbase),
+               "s"(n), "n"(kAbove)
+               : "memory", "scc");
+}
+// Waits for every load, if n is 0.
+__device__ __forceinline__ void wait_all_unless(uint32_t n) {
+  asm volatile("s_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 .Lno_wait%=\n\ts_waitcnt vmcnt(0)\n.Lno_wait%=:" ::"s"(n) : "memory", "scc");
+}
+
 template <class Op, class LayoutW, class LayoutX, int kNJ>
 struct TileStream {
   typedef typename Op::Frag Frag;
@@ -584,74 +592,91 @@ struct TileStream {
   static_assert(!LayoutX::transposed || kNJ != 6, "a wave's tokens start on half a panel or on a panel");
   static constexpr int kHJ = kNJ / 2;
   uint8_t* lds;
-  uint32_t o0, o1, o2, o3, o4;  // ring slots: this step's weights and tokens, the next one's, the free one
+  Ring o;
   Frag fa[8], fb[kNJ];
 
   __device__ __forceinline__ void begin(uint8_t* lds_, int nk) {
-    lds = lds_;
-    o0 = 0, o1 = kBlockBytes, o2 = 2 * kBlockBytes, o3 = 3 * kBlockBytes, o4 = 4 * kBlockBytes;
     if (nk > 1)
       wait_vm_and_barrier<kDmaPerThread + kNJ>();
     else
       wait_vm_and_barrier<0>();
+    resume(lds_, Ring{0, kBlockBytes, 2 * kBlockBytes, 3 * kBlockBytes, 4 * kBlockBytes});
+  }
+  __device__ __forceinline__ void resume(uint8_t* lds_, const Ring& ring) {
+    lds = lds_;
+    o = ring;
     const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
     const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * 128), lane);
     const Fragments<LayoutX, Frag> b_lane((uint32_t)((wave >> 1) * 16 * kNJ), lane);
 #pragma unroll
-    for (int j = 0; j < kHJ; ++j) fb[j] = b_lane.read(lds, o1, 0, j * 16);
+    for (int j = 0; j < kHJ; ++j) fb[j] = b_lane.read(lds, o.o1, 0, j * 16);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) fa[i] = a_lane.read(lds, o0, 0, i * 16);
+    for (int i = 0; i < 8; ++i) fa[i] = a_lane.read(lds, o.o0, 0, i * 16);
   }
 
   template <class W, class X, class Tail, class Early, class Late, class Next>
-  __device__ __forceinline__ void run(W& w, X& x, int nk, const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Early&& early, Late&& late,
-                                      Next&& next) {
+  __device__ __forceinline__ uint32_t run(W& w, X& x, int nk, const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Early&& early, Late&& late,
+                                          Next&& next) {
     const int tid = item_thread(), lane = tid & 63, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * 128), lane);
     const Fragments<LayoutX, Frag> b_lane((uint32_t)((wave >> 1) * 16 * kNJ), lane);
     const uint32_t lds_w = lds_addr(lds) + (uint32_t)wave * kDmaPerThread * 1024;
-    const uint32_t lds_x = lds_addr(lds) + (uint32_t)wave * kNJ * 1024;
+    uint32_t lds_x = lds_addr(lds) + (uint32_t)wave * kNJ * 1024;
+    uint32_t follows = kNJ;  // token DMAs of the step that is fetched
     auto read_a = [&](uint32_t slot, int kk, int i) { fa[i] = a_lane.read(lds, slot, kk, i * 16); };
     auto read_b = [&](uint32_t slot, int kk, int j) { fb[j] = b_lane.read(lds, slot, kk, j * 16); };
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int j = 0; j < kNJ; ++j) acc[i][j] = typename Op::Acc{};
-    // Halves and DMAs as in tile_run.
+    // Halves and DMAs as in tile_run.  other: the step that is fetched is the next tile's, if there is one.
     auto w_dma = [](int quarter, int i) { return quarter < 2 && i % 2 == 0 ? quarter * 4 + i / 2 : -1; };
-    auto half0 = [&](auto kkc, auto dma) {
+    auto fetch_w = [&](auto q, auto other) {
+      constexpr int wq = decltype(q)::value;
+      if constexpr (wq >= 0) {
+        if constexpr (decltype(other)::value)
+          dma16_at_m0_if<0>(follows, w.base, w.off[wq]);
+        else
+          dma16_at_m0(w.base, w.off[wq]);
+      }
+    };
+    auto half0 = [&](auto kkc, auto dma, auto other) {
       constexpr int kk = decltype(kkc)::value;
       static_for<8 * kHJ>([&](auto p) {
         constexpr int i = decltype(p)::value / kHJ, j = decltype(p)::value % kHJ;
         constexpr int js = i & 1 ? kHJ - 1 - j : j;
         constexpr int wq = decltype(dma)::value && j == kHJ / 2 ? w_dma(2 * kk, i) : -1;
-        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o4);
+        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o.o4);
         Op::mma(acc[i][js], fa[i], fb[js]);
-        if constexpr (wq >= 0) dma16_at_m0(w.base, w.off[wq]);
-        if constexpr (j == 1 && i < kHJ) read_b(o1, kk, kHJ + i);
+        fetch_w(std::integral_constant<int, wq>{}, other);
+        if constexpr (j == 1 && i < kHJ) read_b(o.o1, kk, kHJ + i);
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    auto half1 = [&](uint32_t sa, uint32_t sb, auto kk1c) {
+    auto half1 = [&](uint32_t sa, uint32_t sb, auto kk1c, auto other) {
       constexpr int kk1 = decltype(kk1c)::value;
       static_for<8 * kHJ>([&](auto p) {
         constexpr int i = decltype(p)::value / kHJ, j = decltype(p)::value % kHJ;
         constexpr int js = kHJ + (i & 1 ? kHJ - 1 - j : j);
-        constexpr bool fetch_x = kk1 == 0 && j == kHJ / 2 && i < kNJ;
+        constexpr bool kOther = decltype(other)::value;
+        constexpr bool fetch_x = kk1 == 0 && j == kHJ / 2 && i < (kOther ? 8 : kNJ);
         constexpr int wq = kk1 == 1 && j == kHJ / 2 ? w_dma(1, i) : -1;
-        if constexpr (fetch_x) dma_m0<i * 1024>(lds_x + o0);
-        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o4);
+        if constexpr (fetch_x) dma_m0<i * 1024>(lds_x + o.o0);
+        if constexpr (wq >= 0) dma_m0<wq * 1024>(lds_w + o.o4);
         Op::mma(acc[i][js], fa[i], fb[js]);
-        if constexpr (fetch_x) dma16_at_m0(x.base, x.off[i]);
-        if constexpr (wq >= 0) dma16_at_m0(w.base, w.off[wq]);
+        if constexpr (fetch_x && kOther)
+          dma16_at_m0_if<i>(follows, x.base, x.off[i]);
+        else if constexpr (fetch_x)
+          dma16_at_m0(x.base, x.off[i]);
+        fetch_w(std::integral_constant<int, wq>{}, other);
         if constexpr (j == 0 && i < kHJ) read_b(sb, kk1, i);
         if constexpr (j == kHJ - 1) read_a(sa, kk1, i);
         __builtin_amdgcn_sched_barrier(0);
       });
     };
     // last: elements past K's end are zeroed.
-    auto step = [&](auto last) {
+    auto step = [&](auto other, auto last) {
       constexpr bool kLast = decltype(last)::value;
       using first = std::integral_constant<int, 0>;
       using second = std::integral_constant<int, 1>;
@@ -665,30 +690,32 @@ struct TileStream {
         if constexpr (kLast) mask_elements(tail, kk, lk, fb, kHJ, kHJ);
       };
       mask0(0);
-      half0(first{}, std::true_type{});
+      half0(first{}, std::true_type{}, other);
       mask1(0);
-      half1(o0, o1, second{});
+      half1(o.o0, o.o1, second{}, other);
       mask0(1);
-      half0(second{}, std::false_type{});
+      half0(second{}, std::false_type{}, other);
       mask1(1);
+      if constexpr (decltype(other)::value) wait_all_unless(follows);
       wait_vm_and_barrier<kDmaPerThread>();  // the next step visible, this one's slots free
-      half1(o2, o3, first{});
-      const uint32_t t0 = o0, t1 = o1;
-      o0 = o2, o1 = o3, o2 = o4, o3 = t0, o4 = t1;
+      half1(o.o2, o.o3, first{}, other);
+      o = Ring{o.o2, o.o3, o.o4, o.o0, o.o1};
     };
     early();
     for (int ks = 0; ks + 2 < nk; ++ks) {
-      step(std::false_type{});
+      step(std::false_type{}, std::false_type{});
       advance_to(w, x, ks + 3, nk, tail);
     }
-    late();
+    follows = (uint32_t)__builtin_amdgcn_readfirstlane((int)late());
+    lds_x = lds_addr(lds) + (uint32_t)wave * follows * 1024;
     if (nk > 1) {
-      step(std::false_type{});
+      step(std::true_type{}, std::false_type{});
       next(1);
     }
-    step(std::true_type{});
+    step(std::true_type{}, std::true_type{});
     next(2);
     mfma_drain(acc);
+    return follows;
   }
   // All waves are done reading LDS before what comes next writes it.
   __device__ __forceinline__ void end() const { wait_vm_and_barrier<0>(); }

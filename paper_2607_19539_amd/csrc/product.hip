@@ -302,19 +302,22 @@ __device__ __forceinline__ void narrow_item(const ProductArgs& a, Item& it, Prod
   it = next;
 }
 
-// Tiles of 32 kDma rows one after another, as long as the next item is as high, the first one started by `src`.  Leaves
-// the next item in `it`, started.
+// Tiles of 32 kDma rows one after another, as long as the next item is as high.  The first is started by `src`, or
+// (`running`) by the tile before it, in its ring.  Leaves the next item in `it`, started; true: in the ring.
 template <bool by_k, int kDma, class Find>
-__device__ __forceinline__ void tall_items(const ProductArgs& a, Item& it, ProductSource<by_k>& src, uint8_t* lds, Find&& find) {
+__device__ __forceinline__ bool tall_items(const ProductArgs& a, Item& it, ProductSource<by_k>& src, uint8_t* lds, Ring& ring, bool running,
+                                           Find&& find) {
   const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
   auto quad_n = [&](int i) { return (wave & 1) * 128 + i * 16; };
   auto quad_m = [&](int j, int lane) { return (wave >> 1) * (16 * kDma) + j * 16 + (lane & 15); };
   const ElementTail tail = tail_of<by_k>(a);
   const int nk = ElementTail::steps(a.K);
-  DmaRows<kDma> x = src.template first_rows<kDma>();
   TileStream<Bf16Mma, WeightLayout<by_k>, ByRow, kDma> stream;
-  stream.begin(lds, nk);
-  bool follows;
+  if (running)
+    stream.resume(lds, ring);
+  else
+    stream.begin(lds, nk);
+  uint32_t follows;
   do {
     f32x4 acc[8][kDma];
     uint32_t r[kDma];
@@ -324,22 +327,20 @@ __device__ __forceinline__ void tall_items(const ProductArgs& a, Item& it, Produ
       next = find();
       if (next.rows > 0) src.rows(a, next);
     };
+    // Another tall tile may follow in the ring.
     auto late = [&] {
       arrived(r);
-      follows = nk > 1 && next.rows > 0 && row_dmas(next.rows) == kDma;
-      if (follows) {
+      const int dma = nk > 1 && next.rows > 64 ? row_dmas(next.rows) : 0;
+      if (dma > 0) {
         src.addresses(a, next);
-        x = src.template first_rows<kDma>();
-        advance_to(src.w, x, 0, nk, tail);
-      } else {
-        step_back(src.w);
-        step_back(x);
+        advance_to(src.w, src.x, 0, nk, tail);
       }
+      return dma;
     };
-    stream.run(src.w, x, nk, tail, acc, early, late, [&](int k) {
-      if (follows) advance_to(src.w, x, k, nk, tail);
+    follows = stream.run(src.w, src.x, nk, tail, acc, early, late, [&](int k) {
+      if (nk > 1 && next.rows > 64) advance_to(src.w, src.x, k, nk, tail);
     });
-    if (!follows) {
+    if (follows == 0) {
       stream.end();
       if (next.rows > 0) {
         src.addresses(a, next);
@@ -348,7 +349,9 @@ __device__ __forceinline__ void tall_items(const ProductArgs& a, Item& it, Produ
     }
     store_tile<true>(a, it, acc, r, quad_n, quad_m);
     it = next;
-  } while (follows);
+  } while (follows == kDma);
+  ring = stream.o;
+  return follows > 0;
 }
 
 // Workgroups that stay: b takes item (b / 8 + 7 n) mod (workgroups of its XCD) of the n-th set that its XCD's
@@ -371,13 +374,15 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
   src.rows(a, it);
   src.addresses(a, it);
   src.start(a, it, lds);
+  Ring ring{};
+  bool running = false;
   while (it.rows > 0) {
     switch (row_dmas(it.rows)) {
       case 1: narrow_item<by_k, 1>(a, it, src, lds, find); break;
       case 2: narrow_item<by_k, 2>(a, it, src, lds, find); break;
-      case 4: tall_items<by_k, 4>(a, it, src, lds, find); break;
-      case 6: tall_items<by_k, 6>(a, it, src, lds, find); break;
-      default: tall_items<by_k, 8>(a, it, src, lds, find); break;
+      case 4: running = tall_items<by_k, 4>(a, it, src, lds, ring, running, find); break;
+      case 6: running = tall_items<by_k, 6>(a, it, src, lds, ring, running, find); break;
+      default: running = tall_items<by_k, 8>(a, it, src, lds, ring, running, find); break;
     }
   }
 }
