@@ -142,10 +142,24 @@ struct DmaRows {
 };
 
 // An operand ByK whose k are rows of a matrix that an index names, the item's from index[0] on.  Block row i of the K
-// step is k, and a lane's DMAs take those from `first` on, 8 apart.  The wave holds the rows of up to eight K steps, a
-// k a lane, and passes a step's around as it comes: the load behind them makes the compiler wait for every DMA as
-// well, which it cannot count, once in eight steps.
-constexpr int kIndexSteps = 8;
+// step is k, and a lane's DMAs take those from `first` on, 8 apart.  The wave holds the rows of up to sixteen K steps, a
+// k a lane, and passes a step's around as it comes.  The loads behind them make the compiler wait for every DMA as
+// well, which it cannot count, once in so many steps; a tile's first ones may be asked for in the tile before it.
+constexpr int kIndexSteps = 16;
+struct IndexAhead {
+  int32_t row[kIndexSteps];
+  // From K step `step` of the n entries of index; the last step starts early, as ElementTail has it, or repeats the
+  // last row.
+  __device__ __forceinline__ void load(const int32_t* index, int n, int step) {
+    const int lane = (int)(threadIdx.x & 63);
+#pragma unroll
+    for (int u = 0; u < kIndexSteps; ++u) row[u] = index[min(min((step + u) * kTileK, max(n - kTileK, 0)) + lane, n - 1)];
+  }
+  __device__ __forceinline__ void arrived() {  // waited for here: later waits for one each would wait for the DMAs between them
+#pragma unroll
+    for (int u = 0; u < kIndexSteps; ++u) asm volatile("" : "+v"(row[u]));
+  }
+};
 template <int kDma>
 struct IndexedRows {
   const uint8_t* base;       // at the tile's first output row
@@ -156,25 +170,28 @@ struct IndexedRows {
   uint32_t chunk[2];         // the lane's chunk in even and odd DMAs
   int first;                 // block row of the lane's first DMA
   bool bad;                  // an entry outside the matrix was met (its row 0 is taken instead)
-  int32_t ahead[kIndexSteps];
-  __device__ __forceinline__ void to(int step) {
-    const int lane = (int)(threadIdx.x & 63);
-    if (step % kIndexSteps == 0) {
-      // The last step starts early, as ElementTail has it, or repeats the last row.
+  IndexAhead ahead;
+  int asked[kDma];
+  // The rows of step 0 (whose entries are in `ahead`) or of the step after the last one asked for ...
+  __device__ __forceinline__ void ask(int step) {
+    if (step > 0) {
+      if (step % kIndexSteps == 0) {
+        ahead.load(index, n, step);
+        ahead.arrived();
+      } else {
 #pragma unroll
-      for (int u = 0; u < kIndexSteps; ++u) ahead[u] = index[min(min((step + u) * kTileK, max(n - kTileK, 0)) + lane, n - 1)];
-      // All of them are waited for here: later waits for one each would wait for the DMAs between them.
-#pragma unroll
-      for (int u = 0; u < kIndexSteps; ++u) asm volatile("" : "+v"(ahead[u]));
-    } else {
-#pragma unroll
-      for (int u = 0; u + 1 < kIndexSteps; ++u) ahead[u] = ahead[u + 1];
+        for (int u = 0; u + 1 < kIndexSteps; ++u) ahead.row[u] = ahead.row[u + 1];
+      }
     }
-    bad |= (uint32_t)ahead[0] >= limit;
-    const int row = (uint32_t)ahead[0] < limit ? ahead[0] : 0;
+    bad |= (uint32_t)ahead.row[0] >= limit;
+    const int row = (uint32_t)ahead.row[0] < limit ? ahead.row[0] : 0;
 #pragma unroll
-    for (int q = 0; q < kDma; ++q)
-      off[q] = (uint32_t)__builtin_amdgcn_ds_bpermute((first + 8 * q) * 4, row) * stride + chunk[q & 1];
+    for (int q = 0; q < kDma; ++q) asked[q] = __builtin_amdgcn_ds_bpermute((first + 8 * q) * 4, row);
+  }
+  // ... and their addresses, when they have come.
+  __device__ __forceinline__ void take() {
+#pragma unroll
+    for (int q = 0; q < kDma; ++q) off[q] = (uint32_t)asked[q] * stride + chunk[q & 1];
   }
 };
 
@@ -278,8 +295,6 @@ struct ChunkTail {  // int8
     lo = (int)back / 16;
     hi = K >= kRowBytes ? 8 : K / 16;
   }
-  __device__ __forceinline__ uint32_t back_w() const { return back; }
-  __device__ __forceinline__ uint32_t back_x() const { return back; }
 };
 // ElementTail: at any element of 2 bytes.  The last K step starts `back` elements early, where K is a whole number of
 // chunks and fills a step, so that no row is read past its end; else the lanes past the end read something else of
@@ -342,35 +357,41 @@ __device__ __forceinline__ void mask_elements(const Tail& tail, int kk, int lk, 
   }
 }
 
-// An operand's source at K step `next`, one step on from where it was.
+// An operand's source at K step `next`, one step on from where it was, in two parts: what has to be asked for, and
+// the move itself, which starts early at the last of nk steps, where its rows do not say so themselves.
 template <int kDma>
-__device__ __forceinline__ void next_step(DmaRows<kDma>& r, int) {
-  r.base += r.step;
+__device__ __forceinline__ void ask_step(DmaRows<kDma>&, int) {}
+template <int kDma>
+__device__ __forceinline__ void ask_step(IndexedRows<kDma>& r, int next) {
+  r.ask(next);
 }
 template <int kDma>
-__device__ __forceinline__ void next_step(IndexedRows<kDma>& r, int next) {
-  r.to(next);
-}
-
-// A last K step that starts early.
-template <int kDma>
-__device__ __forceinline__ void start_early(DmaRows<kDma>& r, uint32_t bytes) {
-  r.base -= bytes;
+__device__ __forceinline__ void take_step(DmaRows<kDma>& r, int next, int nk, uint32_t back) {
+  if (next > 0) r.base += r.step;
+  if (next == nk - 1) r.base -= back;
 }
 template <int kDma>
-__device__ __forceinline__ void start_early(IndexedRows<kDma>&, uint32_t) {}  // as its rows say
+__device__ __forceinline__ void take_step(IndexedRows<kDma>& r, int, int, uint32_t) {
+  r.take();
+}
 
 // Moves both operands to K step `next` of nk, one step on (none before the first).
 template <class W, class X, class Tail>
 __device__ __forceinline__ void advance_to(W& w, X& x, int next, int nk, const Tail& tail) {
-  if (next > 0) {
-    next_step(w, next);
-    next_step(x, next);
-  }
-  if constexpr (Tail::partial) {
-    if (next == nk - 1) {
-      start_early(w, tail.back_w());
-      start_early(x, tail.back_x());
+  if constexpr (std::is_same_v<Tail, ElementTail>) {
+    ask_step(w, next);
+    take_step(w, next, nk, tail.back_w());
+    take_step(x, next, nk, tail.back_x());
+  } else {
+    if (next > 0) {
+      w.base += w.step;
+      x.base += x.step;
+    }
+    if constexpr (Tail::partial) {
+      if (next == nk - 1) {
+        w.base -= tail.back;
+        x.base -= tail.back;
+      }
     }
   }
 }
@@ -563,14 +584,20 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRow
 // under the epilogue the ring is filled anew for each tile, by all compute units at once.)
 //   begin   after tile_start: a ring of its own
 //   resume  the ring as the tile before left it, which has fetched the first two steps of this one
-//   run     the K loop.  early(): before the first step.  late(): two K steps before the end (or one); it gives the token
-//           DMAs of the tile that follows, 4, 6 or 8, whose first step w and x then are at, and next(k) moves them to its
-//           step k; or 0 where none does.
+//   run     the K loop.  early(): before the first step.  late(): two K steps before the end (or one); it gives the tile
+//           that follows, whose first step w and x then are at.
 //   end     where none follows
 // K has two steps or more where a tile follows, and so has that one.
 // ---------------------------------------------------------------------------
 struct Ring {
   uint32_t o0, o1, o2, o3, o4;  // slots: this step's weights and tokens, the next one's, the free one
+};
+
+template <class Tail>
+struct Following {
+  uint32_t dma;  // its token DMAs, 4, 6 or 8; 0: there is none
+  int nk;        // its K steps
+  Tail tail;
 };
 
 // The DMA at M0, if n > kAbove.  A branch that the compiler does not see: between its own it would move accumulators.
@@ -614,9 +641,8 @@ struct TileStream {
     for (int i = 0; i < 8; ++i) fa[i] = a_lane.read(lds, o.o0, 0, i * 16);
   }
 
-  template <class W, class X, class Tail, class Early, class Late, class Next>
-  __device__ __forceinline__ uint32_t run(W& w, X& x, int nk, const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Early&& early, Late&& late,
-                                          Next&& next) {
+  template <class W, class X, class Tail, class Early, class Late>
+  __device__ __forceinline__ uint32_t run(W& w, X& x, int nk, const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Early&& early, Late&& late) {
     const int tid = item_thread(), lane = tid & 63, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Fragments<LayoutW, Frag> a_lane((uint32_t)((wave & 1) * 128), lane);
@@ -675,8 +701,9 @@ struct TileStream {
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    // last: elements past K's end are zeroed.
-    auto step = [&](auto other, auto last) {
+    // last: elements past K's end are zeroed.  The operands go to step `to` of a tile of nk_to steps, where there is one:
+    // the weights when their DMAs are out, in two parts under the third quarter, the tokens at the end.
+    auto step = [&](auto other, auto last, int to, int nk_to, const Tail& tail_to) {
       constexpr bool kLast = decltype(last)::value;
       using first = std::integral_constant<int, 0>;
       using second = std::integral_constant<int, 1>;
@@ -694,26 +721,23 @@ struct TileStream {
       mask1(0);
       half1(o.o0, o.o1, second{}, other);
       mask0(1);
+      if (follows > 0) ask_step(w, to);
       half0(second{}, std::false_type{}, other);
+      if (follows > 0) take_step(w, to, nk_to, tail_to.back_w());
       mask1(1);
       if constexpr (decltype(other)::value) wait_all_unless(follows);
       wait_vm_and_barrier<kDmaPerThread>();  // the next step visible, this one's slots free
       half1(o.o2, o.o3, first{}, other);
+      if (follows > 0) take_step(x, to, nk_to, tail_to.back_x());
       o = Ring{o.o2, o.o3, o.o4, o.o0, o.o1};
     };
     early();
-    for (int ks = 0; ks + 2 < nk; ++ks) {
-      step(std::false_type{}, std::false_type{});
-      advance_to(w, x, ks + 3, nk, tail);
-    }
-    follows = (uint32_t)__builtin_amdgcn_readfirstlane((int)late());
+    for (int ks = 0; ks + 2 < nk; ++ks) step(std::false_type{}, std::false_type{}, ks + 3, nk, tail);
+    const Following<Tail> f = late();
+    follows = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.dma);
     lds_x = lds_addr(lds) + (uint32_t)wave * follows * 1024;
-    if (nk > 1) {
-      step(std::true_type{}, std::false_type{});
-      next(1);
-    }
-    step(std::true_type{}, std::true_type{});
-    next(2);
+    if (nk > 1) step(std::true_type{}, std::false_type{}, 1, f.nk, f.tail);
+    step(std::true_type{}, std::true_type{}, 2, f.nk, f.tail);
     mfma_drain(acc);
     return follows;
   }

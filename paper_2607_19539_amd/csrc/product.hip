@@ -335,11 +335,9 @@ __device__ __forceinline__ bool tall_items(const ProductArgs& a, Item& it, Produ
         src.addresses(a, next);
         advance_to(src.w, src.x, 0, nk, tail);
       }
-      return dma;
+      return Following<ElementTail>{(uint32_t)dma, nk, tail};
     };
-    follows = stream.run(src.w, src.x, nk, tail, acc, early, late, [&](int k) {
-      if (nk > 1 && next.rows > 64) advance_to(src.w, src.x, k, nk, tail);
-    });
+    follows = stream.run(src.w, src.x, nk, tail, acc, early, late);
     if (follows == 0) {
       stream.end();
       if (next.rows > 0) {

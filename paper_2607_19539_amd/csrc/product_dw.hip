@@ -98,11 +98,11 @@ template <bool indexed, int kDma>
 using XRows = std::conditional_t<indexed, IndexedRows<kDma>, DmaRows<kDma>>;
 
 template <int kDma>
-__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, DmaRows<kDma>& d) {
+__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, const IndexAhead&, DmaRows<kDma>& d) {
   rows_by_k(a.x, a.K, it, it.k0, lane, wave, d);
 }
 template <int kDma>
-__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, IndexedRows<kDma>& d) {
+__device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, const IndexAhead& ahead, IndexedRows<kDma>& d) {
   const int panel = wave * kDma / 8;
   d.base = a.x_rows > 0 ? (const uint8_t*)(a.x + it.k0) : (const uint8_t*)a.dy;
   d.index = a.index + it.row0;
@@ -117,9 +117,17 @@ __device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it,
     const int col = min(it.k0 + panel * 64 + (int)((((uint32_t)lane & 7) ^ swz_k(k)) << 3), a.K - 8) - it.k0;
     d.chunk[h] = (uint32_t)col * 2;
   }
-  d.to(0);
+  d.ahead = ahead;
+  d.ahead.arrived();
+  d.ask(0);
+  d.take();
 #pragma unroll
   for (int i = 0; i < kDma; ++i) asm volatile("" ::"v"(d.off[i]));  // complete before the first DMA
+}
+// What x_rows needs from memory.
+template <bool indexed>
+__device__ __forceinline__ void x_ahead(const ProductDwArgs& a, const DwItem& it, IndexAhead& ahead) {
+  if constexpr (indexed) ahead.load(a.index + it.row0, it.rows, 0);
 }
 
 // Where the sum over an item's rows ends.  An index starts its last step early by itself.
@@ -177,7 +185,9 @@ __global__ __launch_bounds__(kThreads, kTile <= 64 ? 4 : 2) void dw_small_kernel
   if (it.rows > 0) {
     XRows<indexed, kN> x;
     DmaRows<kN> y;
-    x_rows(a, it, lane, wave, x);
+    IndexAhead ahead;
+    x_ahead<indexed>(a, it, ahead);
+    x_rows(a, it, lane, wave, ahead, x);
     rows_by_k(a.dy, a.N, it, it.n0, lane, wave, y);
     small_mma<Bf16Mma, kTile, kTile, kStages, ByK, ByK>(lds, x, y, it.rows, tail_of<indexed>(a, it.rows), acc);
     if constexpr (indexed) bad = __syncthreads_or(any_bad(x));  // a wave has met a part of the rows
@@ -203,51 +213,50 @@ template <bool indexed>
 struct DwSource {
   XRows<indexed, kDmaPerThread> x;
   DmaRows<8> y;
-  __device__ __forceinline__ void start(const ProductDwArgs& a, const DwItem& it, uint8_t* lds) {
+  IndexAhead ahead;  // of the tile whose addresses come next
+  __device__ __forceinline__ void rows(const ProductDwArgs& a, const DwItem& it) { x_ahead<indexed>(a, it, ahead); }
+  // 8 or 4 token DMAs: tiles of 256 n, and of the 128 or fewer that are left.
+  static __device__ __forceinline__ int dmas(const ProductDwArgs& a, const DwItem& it) { return a.N - it.n0 > 128 ? 8 : 4; }
+  __device__ __forceinline__ void addresses(const ProductDwArgs& a, const DwItem& it) {
     const int lane = item_thread() & 63, wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
-    const ElementTail tail = tail_of<indexed>(a, it.rows);
-    x_rows(a, it, lane, wave, x);
-    if (a.N - it.n0 > 128) {
+    x_rows(a, it, lane, wave, ahead, x);
+    if (dmas(a, it) == 8) {
       rows_by_k(a.dy, a.N, it, it.n0, lane, wave, y);
+    } else {
+      const auto half = first_dmas<4>();
+      DmaRows<4> h = half;
+      rows_by_k(a.dy, a.N, it, it.n0, lane, wave, h);
+      y.base = h.base;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y.off[i] = h.off[i];
+    }
+    y.step = (uint32_t)kTileK * (uint32_t)a.N * 2;
+  }
+  template <int kDma>
+  __device__ __forceinline__ DmaRows<kDma> first_dmas() const {
+    DmaRows<kDma> r{y.base, y.step, {}};
+#pragma unroll
+    for (int i = 0; i < kDma; ++i) r.off[i] = y.off[i];
+    return r;
+  }
+  // The first K steps on their way, the bases at the step after them.
+  __device__ __forceinline__ void start(const ProductDwArgs& a, const DwItem& it, uint8_t* lds) {
+    const ElementTail tail = tail_of<indexed>(a, it.rows);
+    if (dmas(a, it) == 8) {
       tile_start<8>(lds, x, y, it.rows, tail);
     } else {
-      DmaRows<4> half;
-      rows_by_k(a.dy, a.N, it, it.n0, lane, wave, half);
+      auto half = first_dmas<4>();
       tile_start<4>(lds, x, half, it.rows, tail);
       y.base = half.base;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y.off[i] = half.off[i];
     }
   }
 };
 
-// The K loop and the epilogue of a tile of 256 k by 32 kDma n, whose first K steps `src` has started.  Those of the next
-// item, which find() gives, are started between the two.
-template <bool indexed, int kDma, class Find>
-__device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, const DwItem& it, DwItem& next, DwSource<indexed>& src,
-                                             uint8_t* lds, Find&& find) {
+// The finished tile.  One that lies within dw, and replaces it, is stored without a question.
+template <int kDma>
+__device__ __forceinline__ void store_dw_tile(const ProductDwArgs& a, int split, const DwItem& it, f32x4 (&acc)[8][kDma], bool bad) {
   const int wave = __builtin_amdgcn_readfirstlane(item_thread() >> 6);
-  f32x4 acc[8][kDma];
-  bool bad = false;
-  if (it.rows > 0) {
-    DmaRows<kDma> y{src.y.base, (uint32_t)kTileK * (uint32_t)a.N * 2, {}};
-#pragma unroll
-    for (int i = 0; i < kDma; ++i) y.off[i] = src.y.off[i];
-    tile_run<Bf16Mma, ByK, ByK>(lds, src.x, y, it.rows, tail_of<indexed>(a, it.rows), acc, [&] { next = find(); }, [] {});
-    bad = any_bad(src.x);  // every wave has met every row
-  } else {
-    next = find();
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int j = 0; j < kDma; ++j) {
-        acc[i][j] = f32x4{};
-        asm volatile("" : "+a"(acc[i][j]));
-      }
-  }
-  if (next.rows > 0) src.start(a, next, lds);
   const int lane = item_thread() & 63, lr = lane & 15, lk = lane >> 4;
-  // A tile that lies within dw, and replaces it, is stored without a question: the others' cost a tile 2 us.
   auto store = [&](auto plain) {
     constexpr bool kPlain = decltype(plain)::value;
 #pragma unroll
@@ -276,6 +285,54 @@ __device__ __forceinline__ void dw_tile_item(const ProductDwArgs& a, int split, 
     store(std::false_type{});
 }
 
+// An item without rows: zeros.
+__device__ __forceinline__ void no_rows(const ProductDwArgs& a, int split, const DwItem& it) {
+  const int tid = item_thread();
+  for (int i = tid; i < 256 * 64; i += kThreads) store_inside(a, it, split, it.n0 + i / 64, it.k0 + i % 64 * 4, f32x4{});
+}
+
+// Tiles of 256 k by 32 kDma n one after another, as long as the next item has rows and is as wide.  The first is started
+// by `src`, or (`running`) by the tile before it, in its ring.  Leaves the next item in `it`, started if it has rows;
+// true: in the ring.
+template <bool indexed, int kDma, class Find>
+__device__ __forceinline__ bool dw_tiles(const ProductDwArgs& a, int split, DwItem& it, DwSource<indexed>& src, uint8_t* lds, Ring& ring,
+                                         bool running, Find&& find) {
+  TileStream<Bf16Mma, ByK, ByK, kDma> stream;
+  if (running)
+    stream.resume(lds, ring);
+  else
+    stream.begin(lds, ElementTail::steps(it.rows));
+  uint32_t follows;
+  do {
+    f32x4 acc[8][kDma];
+    const int nk = ElementTail::steps(it.rows);
+    DwItem next;
+    bool bad = false;
+    auto early = [&] {
+      next = find();
+      if (next.rows > 0) src.rows(a, next);
+    };
+    auto late = [&] {
+      bad = any_bad(src.x);  // every wave has asked for every row, but for ...
+      const bool fits = nk > 1 && next.rows > kTileK;
+      if (fits) src.addresses(a, next);
+      return Following<ElementTail>{fits ? (uint32_t)src.dmas(a, next) : 0u, ElementTail::steps(next.rows), tail_of<indexed>(a, next.rows)};
+    };
+    follows = stream.run(src.x, src.y, nk, tail_of<indexed>(a, it.rows), acc, early, late);
+    if (follows == 0) {
+      stream.end();
+      if (next.rows > 0) {
+        src.addresses(a, next);
+        src.start(a, next, lds);
+      }
+    }
+    store_dw_tile(a, split, it, acc, bad);
+    it = next;
+  } while (follows == kDma);
+  ring = stream.o;
+  return follows > 0;
+}
+
 // Workgroups that stay, a compute unit each; the 32 of an XCD take runs of consecutive items.
 template <bool indexed>
 __global__ __launch_bounds__(kThreads, 1) void dw_tile_kernel(ProductDwArgs a, int split) {
@@ -290,14 +347,25 @@ __global__ __launch_bounds__(kThreads, 1) void dw_tile_kernel(ProductDwArgs a, i
   };
   DwItem it = find();
   DwSource<indexed> src;
-  if (it.rows > 0) src.start(a, it, lds);
+  Ring ring{};
+  bool running = false, started = false;
   while (it.expert >= 0) {
-    DwItem next;
-    if (a.N - it.n0 > 128)
-      dw_tile_item<indexed, 8>(a, split, it, next, src, lds, find);
+    if (it.rows <= 0) {
+      no_rows(a, split, it);
+      it = find();
+      started = false;
+      continue;
+    }
+    if (!started) {
+      src.rows(a, it);
+      src.addresses(a, it);
+      src.start(a, it, lds);
+    }
+    started = true;  // what follows a tile is started by it
+    if (src.dmas(a, it) == 8)
+      running = dw_tiles<indexed, 8>(a, split, it, src, lds, ring, running, find);
     else
-      dw_tile_item<indexed, 4>(a, split, it, next, src, lds, find);
-    it = next;
+      running = dw_tiles<indexed, 4>(a, split, it, src, lds, ring, running, find);
   }
 }
 
