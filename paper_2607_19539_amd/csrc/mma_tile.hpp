@@ -128,6 +128,15 @@ __device__ __forceinline__ void wait_vm_and_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// The same of this wave's loads alone, without the barrier.
+template <int n>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(n >= 0 && n < 64, "vmcnt range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (0 << 8));
+  asm volatile("" ::: "memory");
+}
+
 // One operand of an item as a DMA source.  Instruction i of a wave fetches 8 rows: lane l the 16 bytes
 // at base + off[i], its row's (l / 8) 16-byte chunk that belongs at its slot in LDS.  The scalar base
 // advances by `step` per K step, so a DMA costs two instructions beside the matrix ones: with a

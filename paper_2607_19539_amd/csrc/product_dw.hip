@@ -403,26 +403,29 @@ hipError_t launch_dw(const DwPlan& plan, const ProductDwArgs& a, hipStream_t s) 
 }  // namespace
 
 DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N) {
-  // What each way would take, in microseconds, from the rows an expert has on average: rounds of tiles over as many
-  // workgroups as run at once, each so many K steps and something for its start and its end, the writing of the sums,
-  // and the second launch that adds up parts.  Fitted to 2106 measured sums of 400 problems (1 to 49152 rows, 1 to 128
-  // experts): the way chosen takes 3 % longer than the best one, 19 % in one of twenty.
+  // What each way would take, in microseconds, from the rows an expert has on average: one tile alone, or as many as a
+  // compute unit has one after another, whichever is longer; the writing of the sums; and the second launch that adds up
+  // parts.  Fitted to 3236 problems (1 to 49152 rows, 1 to 128 experts): the way chosen takes 2.7 % longer than the best
+  // one, 18 % in one of twenty, 59 % at most.
   const double nk = std::ceil((double)rows / experts / kTileK), megabytes = (double)experts * N * K * 4e-6;
   DwPlan best{256, 1};
   double least = 1e30;
-  auto consider = [&](int tile, double at_once, double step, double fixed, double write, double start, double waste, double join) {
-    const double tiles = (double)experts * std::ceil((double)N / tile) * std::ceil((double)K / tile) / at_once;
+  struct Cost {
+    double step_alone, alone, step, each, waste, write, start, join, second;
+  };
+  auto consider = [&](int tile, const Cost& c) {
+    const double tiles = (double)experts * std::ceil((double)N / tile) * std::ceil((double)K / tile) / 256;
     for (int split = 1; split <= 32; split *= 2) {
       if (split > 1 && (nk < split || split * megabytes > 1024)) break;
-      const double items = tiles * split, rounds = items < 1 ? 1 : items + waste * (std::ceil(items) - items);
-      const double cost = start + rounds * (std::ceil(nk / split) * step + fixed) + megabytes * split * write +
-                          (split > 1 ? 1 + megabytes * split * join : 0);
+      const double items = tiles * split, rounds = items + c.waste * (std::ceil(items) - items), steps = std::ceil(nk / split);
+      const double cost = c.start + std::max(steps * c.step_alone + c.alone, rounds * (steps * c.step + c.each)) + megabytes * split * c.write +
+                          (split > 1 ? c.second + megabytes * split * c.join : 0);
       if (cost < least) best = DwPlan{tile, split}, least = cost;
     }
   };
-  consider(256, 256, 1.11, 7.6, 0.072, 4.6, 0.86, 0.25);
-  consider(128, 512, 0.97, 1.5, 0.147, 3.1, 0.84, 0.28);
-  consider(64, 1024, 0.91, 0, 0.21, 2.9, 0.14, 0.23);
+  consider(256, {0.505, 1.7, 1.1, 8.6, 0.88, 0.056, 6.0, 0.224, 1.4});
+  consider(128, {0.615, 0.6, 0.578, 0.5, 0.39, 0.154, 4.6, 0.246, 1.6});
+  consider(64, {0.413, 0, 0.244, 0.55, 1, 0.072, 3.2, 0.196, 2.4});
   return best;
 }
 

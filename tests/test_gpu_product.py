@@ -188,7 +188,7 @@ def test_each_product_kernel(counts, K, N, kind, gather):
         d["index"][d["rows"] // 2], d["index"][1] = -5, d["n"]
         d["index_dev"] = torch.from_numpy(d["index"]).cuda()
     check_rows(launch_kind(kind, d, False), d, lambda r: x_rows(d, r), N, "rows")
-    if not kind.startswith("slim") and not gather:
+    if not gather:
         check_rows(launch_kind(kind, d, True), d, lambda r: d["dy"][r], K, "k")
         # With the matrix the other way round, so that the long side is summed over and the short one comes out.
         t = case(counts, N, K, False, K * 5 + N)
@@ -226,7 +226,7 @@ def test_a_row_that_is_not_there_shows_in_its_experts_dw(tile, split):
     check_dw(host(dw), d)
 
 
-@pytest.mark.parametrize("kind", KINDS[2:])
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("K", [40, 72, 200])
 def test_values_past_the_end_of_a_sum_do_not_enter_it(K, kind):
     """Infinities and NaN of other rows and other experts, and an infinity that a sum's last step would meet twice."""

@@ -182,7 +182,7 @@ def test_the_product_chosen_can_be_launched(rows, grouped, E, K, N, by_k):
     f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_bool] + [ctypes.c_int32] * 3 + [ctypes.c_bool], ctypes.c_int
     kind, ends = f(rows, grouped, E, K, N, by_k), E if grouped else 0
     if kind < 2:
-        assert not by_k and -(-rows // 16) + ends <= 65535 and -(-N // (16 << kind)) * 256 < 2 ** 32
+        assert -(-rows // 16) + ends <= 65535 and -(-N // (64 if by_k else 16 << kind)) * 256 < 2 ** 32
     elif kind < 4:
         side = 64 if kind == 2 else 128
         assert (-(-rows // side) + ends) * -(-N // side) * 256 < 2 ** 32
