@@ -104,7 +104,7 @@ __device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it,
 template <int kDma>
 __device__ __forceinline__ void x_rows(const ProductDwArgs& a, const DwItem& it, int lane, int wave, const IndexAhead& ahead, IndexedRows<kDma>& d) {
   const int panel = wave * kDma / 8;
-  d.base = a.x_rows > 0 ? (const uint8_t*)(a.x + it.k0) : (const uint8_t*)a.dy;
+  d.base = a.x_rows > 0 ? (const uint8_t*)(a.x + it.k0) : (const uint8_t*)a.dw;  // which has a row of K as well
   d.index = a.index + it.row0;
   d.n = it.rows;
   d.limit = (uint32_t)a.x_rows;
@@ -416,6 +416,7 @@ DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N) {
   auto consider = [&](int tile, const Cost& c) {
     const double tiles = (double)experts * std::ceil((double)N / tile) * std::ceil((double)K / tile) / 256;
     for (int split = 1; split <= 32; split *= 2) {
+      if (tile != 256 && tiles * split * 256 * kThreads > UINT32_MAX) break;  // more than one launch takes
       if (split > 1 && (nk < split || split * megabytes > 1024)) break;
       const double items = tiles * split, rounds = items + c.waste * (std::ceil(items) - items), steps = std::ceil(nk / split);
       const double cost = c.start + std::max(steps * c.step_alone + c.alone, rounds * (steps * c.step + c.each)) + megabytes * split * c.write +

@@ -357,6 +357,19 @@ def test_tensors_past_4_gib():
     assert bool((x[rows - 1] == 8 * 4096).all()) and not bool(x[:rows - 1].any())
 
 
+@pytest.mark.parametrize("rows,K,N", [(2, 8, 8), (70, 264, 72), (600, 512, 256)])
+def test_an_index_into_no_rows(rows, K, N):
+    """Every entry of row_index is outside: NaN, and nothing is read past a tensor."""
+    x = torch.zeros((0, K), dtype=torch.bfloat16, device="cuda")
+    index = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(0)
+    w, dy = torch.randn((1, N, K), generator=g).to(torch.bfloat16).cuda(), torch.randn((rows, N), generator=g).to(torch.bfloat16).cuda()
+    y, dw = filled((rows, N)), filled((1, N, K), torch.float32)
+    B.moe_product(x, w, y, row_index=index)
+    B.moe_product_dw(dy, x, dw, row_index=index)
+    assert bool(y.isnan().all()) and bool(dw.isnan().all())
+
+
 def test_no_rows():
     w, none = filled((2, 16, 8)), torch.zeros((0, 8), dtype=torch.bfloat16, device="cuda")
     off, dy = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros((0, 16), dtype=torch.bfloat16, device="cuda")

@@ -186,3 +186,14 @@ def test_the_product_chosen_can_be_launched(rows, grouped, E, K, N, by_k):
     elif kind < 4:
         side = 64 if kind == 2 else 128
         assert (-(-rows // side) + ends) * -(-N // side) * 256 < 2 ** 32
+
+
+@pytest.mark.parametrize("rows,E,K,N", [(1, 1024, 2 ** 13, 2 ** 13), (64, 1, 2 ** 18, 2 ** 18), (2 ** 31 - 1, 1, 2 ** 18, 2 ** 18), (1, 1, 2 ** 18, 2 ** 17)])
+def test_the_way_to_dw_can_be_launched(rows, E, K, N):
+    class DwPlan(ctypes.Structure):
+        _fields_ = [("tile", ctypes.c_int), ("split", ctypes.c_int)]
+
+    f = B.load()._ZN3moe15product_dw_planEliii
+    f.argtypes, f.restype = [ctypes.c_int64] + [ctypes.c_int32] * 3, DwPlan
+    p = f(rows, E, K, N)
+    assert p.tile == 256 or E * p.split * -(-N // p.tile) * -(-K // p.tile) * 256 < 2 ** 32
