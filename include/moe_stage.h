@@ -553,7 +553,8 @@ int moe_q8_gated(const void* xq, const float* x_scale, int64_t x_rows, const int
 /* ---------------------------------------------------------------------------
  * What trains a layer of experts: the 16-bit products and their gradients, the
  * gated activation, the combine's gradient, and the norm of all gradients.  They
- * behave as the operators above do.
+ * behave as the operators above do.  (A row of moe_gate has ffn / 8 threads, a
+ * choice of moe_combine_backward 64.)
  * ------------------------------------------------------------------------- */
 
 /*

@@ -3,7 +3,8 @@
 //   drecv[slot[t, j]] = bf16( gate[t, j] dout[t] ),   dgate[t, j] = sum_h dout[t, h] recv[slot[t, j], h]
 //
 // A wave takes one choice of one token: it reads dout's row and recv's, and writes drecv's, 16 bytes a lane.  The choices
-// of a token are next to each other, in one workgroup or on one XCD, so that dout's row comes from memory once.
+// of a token are next to each other, in one workgroup or on one XCD, so that dout's row comes from memory once.  Memory
+// bounds it: 8192 tokens, 6 choices of 2048 features, 437 MB in 89 us (4.9 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
