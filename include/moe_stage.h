@@ -639,8 +639,8 @@ typedef struct {
  *   moe_squares   total = sum over all tensors of v^2          (fp64, in a fixed order)
  *   moe_clip      norm = sqrt(total),  out = v * max_norm / norm where norm > max_norm, else v
  * total and norm (fp32, optional) are device memory.  Between the two calls a program with tensors on other
- * ranks adds up their totals.  A norm that is not finite leaves every value as it is; the caller sees it in
- * norm.  max_norm >= 0.  moe_clip's outs may not overlap each other or another tensor's data (MOE_EINVAL);
+ * ranks adds up their totals.  A norm that is not finite in fp32 leaves every value as it is; the caller sees
+ * it in norm.  max_norm >= 0.  moe_clip's outs may not overlap each other or another tensor's data (MOE_EINVAL);
  * tensors that are their own out are not touched where nothing is scaled.
  * `workspace` holds at least moe_squares_workspace(tensors, n) bytes (8-byte aligned).
  */

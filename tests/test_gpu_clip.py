@@ -150,3 +150,26 @@ def test_an_out_that_overlaps_another_tensor_is_refused():
     B.moe_clip([a, c], total, 1.0)
     B.moe_clip([a, a[:0], c], total, 1.0)
     B.moe_squares([a, a, b], total)
+
+
+@pytest.mark.parametrize("value", [3e38, -3e38])
+def test_a_norm_that_32_bits_do_not_hold_changes_nothing(value):
+    """Finite in 64 bits, infinite in the norm that the caller sees."""
+    tensors = [torch.full((100,), value, device="cuda"), torch.full((64,), 2.0, dtype=BF16, device="cuda")]
+    before, out = [t.clone() for t in tensors], [torch.zeros_like(t) for t in tensors]
+    total, norm = torch.zeros(1, dtype=torch.float64, device="cuda"), torch.zeros(1, device="cuda")
+    B.moe_squares(tensors, total)
+    assert math.isfinite(float(total))
+    B.moe_clip(tensors, total, 1.0, norm=norm, out=out)
+    B.moe_clip(tensors, total, 1.0)
+    assert math.isinf(float(norm))
+    for b, t, o in zip(before, tensors, out):
+        assert torch.equal(b, t) and torch.equal(b, o)
+
+
+@pytest.mark.parametrize("max_norm", [2.0 ** -23, 2.0 ** -30, 2.0 ** -43, 2.0 ** -66])
+def test_a_scale_that_32_bits_hold_as_a_subnormal(max_norm):
+    """From a norm of some 1e33 down: the scale is below 2^-126 but the results are ordinary values."""
+    tensors = make([(5000, F32), (4000, BF16)], 12, 1e31)
+    check([t.clone() for t in tensors], max_norm)
+    check(tensors, max_norm, in_place=True)
