@@ -156,8 +156,11 @@ hipError_t launch_q8_kind(Q8Kind kind, const Q8Args& a, bool gated, hipStream_t 
 hipError_t launch_q8(const Q8Args& a, bool gated, hipStream_t s);
 
 // Which kernel takes a 16-bit product: 16 rows by 16 or 32 features straight from memory, or tiles of 64, 128 or 256
-// features by as many rows through LDS.  by_k: W's columns lie in memory, not its rows.
-enum ProductKind { kProductSlim1, kProductSlim2, kProductTiles64, kProductTiles128, kProductTiles256 };
+// features by as many rows through LDS, of 128 features by 64 rows, or (by_k) of 128 with a deeper ring.  by_k: W's
+// columns lie in memory, not its rows.
+enum ProductKind {
+  kProductSlim1, kProductSlim2, kProductTiles64, kProductTiles128, kProductTiles256, kProductTiles128x64, kProductDeep128
+};
 ProductKind product_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool by_k);
 hipError_t launch_product_kind(ProductKind kind, const ProductArgs& a, bool by_k, hipStream_t s);
 hipError_t launch_product(const ProductArgs& a, bool by_k, hipStream_t s);

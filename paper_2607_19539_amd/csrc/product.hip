@@ -12,7 +12,8 @@
 //    another in the ring.  Their K steps bound them: 8192 rows by 4096 x 14336 take 630 us (1.53 PFLOP/s; the library's
 //    product 613), ByK 616 (1.56; 689).  Ragged experts cost what their short last tiles and the last round leave idle:
 //    64 of some 768 rows by 2816 x 2048 480 us (1.18), 8 of some 1024 by 4096 x 14336 770 (1.25).
-//  * tiles of 128 or 64, bound by their loads, where whole tiles would leave compute units idle.
+//  * tiles of 128 features by 128 or 64 rows, or of 64 each way, bound by their loads, where whole tiles would leave compute
+//    units idle.
 //  * 16 rows by 16, 32 or (ByK) 64 features, K divided among the waves, for a few rows of each expert: bound by the
 //    reading of the weights (32 experts of 4096 x 7168, 8 rows each: 1.88 GB in 310 us, 6.1 TB/s), or by its latency.
 #include <hip/hip_runtime.h>
@@ -80,9 +81,11 @@ __device__ __forceinline__ bool named(const ProductArgs& a, uint32_t r) { return
 
 // K steps in a small tile's ring.  Four, of which a compute unit holds two workgroups with tiles of 64 and one with
 // tiles of 128.  With weights ByK two workgroups of tiles of 128 with two steps each are 5 % faster (290 products of over
-// 40 us; 3 % slower ByRow), since one's reads fill the other's waits.  Tiles of 64 with two steps: 20 to 40 % slower.
-template <bool by_k, int kW>
-constexpr int kStages = by_k && kW == 128 ? 2 : 4;
+// 40 us; 3 % slower ByRow), since one's reads fill the other's waits, except where every compute unit has one tile at most:
+// three steps for it alone take 10 % less there (16 experts of some 180 rows, 1408 x 1024: 22.7 -> 19.6 us).  Tiles of 64
+// with two steps: 20 to 40 % slower.  128 features by 64 rows have three, two workgroups a compute unit.
+template <bool by_k, int kW, int kX>
+constexpr int kStages = kW != kX ? 3 : by_k && kW == 128 ? 2 : 4;
 
 template <int kW, int kX>
 struct SmallShape {
@@ -91,7 +94,7 @@ struct SmallShape {
 };
 
 // One tile of kW features by kX rows, of which it.rows are valid.
-template <bool by_k, int kW, int kX>
+template <bool by_k, int kW, int kX, int kSteps>
 __device__ __forceinline__ void small_item(const ProductArgs& a, const Item& it, uint8_t* lds) {
   using S = SmallShape<kW, kX>;
   constexpr int kNI = kW / 32, kNJ = kX / 32;
@@ -126,7 +129,7 @@ __device__ __forceinline__ void small_item(const ProductArgs& a, const Item& it,
   for (int j = 0; j < kNJ; ++j) asm volatile("" ::"v"((int)ok[j]));
 
   f32x4 acc[kNI][kNJ];
-  small_mma<Bf16Mma, kW, kX, kStages<by_k, kW>, WeightLayout<by_k>>(lds, w, x, K, tail_of<by_k>(a), acc);
+  small_mma<Bf16Mma, kW, kX, kSteps, WeightLayout<by_k>>(lds, w, x, K, tail_of<by_k>(a), acc);
 
 #pragma unroll
   for (int i = 0; i < kNI; ++i)
@@ -149,13 +152,13 @@ __device__ __forceinline__ void small_item(const ProductArgs& a, const Item& it,
   }
 }
 
-template <bool by_k, int kW, int kX>
-__global__ __launch_bounds__(kThreads, (kStages<by_k, kW>) * (kW + kX) <= 512 ? 2 : 1) void product_small_kernel(ProductArgs a, int cols) {
-  constexpr int kRing = kStages<by_k, kW> * (kW + kX) * kRowBytes, kOut = SmallShape<kW, kX>::kOutBytes;
+template <bool by_k, int kW, int kX, int kSteps = kStages<by_k, kW, kX>>
+__global__ __launch_bounds__(kThreads, 2 * kSteps * (kW + kX) * kRowBytes <= kLdsBytes ? 2 : 1) void product_small_kernel(ProductArgs a, int cols) {
+  constexpr int kRing = kSteps * (kW + kX) * kRowBytes, kOut = SmallShape<kW, kX>::kOutBytes;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kRing > kOut ? kRing : kOut];
   const Item it = uniform(Items<kX>(a, cols).find(a, blockIdx.x % kXcds, blockIdx.x / kXcds));
   if (it.rows <= 0) return;
-  small_item<by_k, kW, kX>(a, it, lds);
+  small_item<by_k, kW, kX, kSteps>(a, it, lds);
 }
 
 // ------------------------------------------------------------------------------------ whole tiles
@@ -600,7 +603,7 @@ hipError_t launch_slim(const ProductArgs& a, hipStream_t s) {
   return launch(product_slim_kernel<kN>, dim3((uint32_t)cols, (uint32_t)tiles), dim3(kThreads), 0, s, a);
 }
 
-template <bool by_k, int kW, int kX>
+template <bool by_k, int kW, int kX, int kSteps = kStages<by_k, kW, kX>>
 hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
   const int64_t tiles = most_tiles(a.rows, a.offsets != nullptr, a.experts, kX);
   const int cols = (a.N + kW - 1) / kW;
@@ -609,7 +612,7 @@ hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
   if constexpr (kW == 256)
     return launch(product_tile_kernel<by_k>, dim3((uint32_t)std::min<int64_t>(grid, kStaying)), dim3(kThreads), 0, s, a, cols);
   else
-    return launch(product_small_kernel<by_k, kW, kX>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
+    return launch(product_small_kernel<by_k, kW, kX, kSteps>, dim3((uint32_t)grid), dim3(kThreads), 0, s, a, cols);
 }
 
 }  // namespace
@@ -644,6 +647,13 @@ ProductKind product_kind(int64_t rows, bool grouped, int32_t experts, int32_t K,
   // The small tiles and the slim kernels have a workgroup for each item, and can be too many for one launch.
   auto launches = [&](int w, int x) { return launch_fits(dealt(most_tiles(rows, grouped, experts, x), (N + w - 1) / w), kThreads); };
   if (launches(128, 128)) consider(kProductTiles128, cost(1.2 + std::ceil(half) * (nk * 0.48 + 2.8), 4.9));
+  // Fitted to 2000 more products (64 to 45000 rows, 1 to 64 experts): these two are chosen for a fifth of them ByRow and a
+  // third ByK, which take 5 and 7 % less for it; one in eight and one in five takes over 5 % less, one in 45 and one in 20 more.
+  if (launches(128, 64)) {
+    const double flat = std::ceil(items(128, 64));
+    consider(kProductTiles128x64, by_k ? cost(1.2 + flat * (nk * 0.362 + 0.97), 5.2) : cost(1.7 + flat * (nk * 0.283 + 1.32), 4.9));
+  }
+  if (by_k && launches(128, 128)) consider(kProductDeep128, cost(0.24 + std::ceil(half) * (nk * 0.46 + 3.75), 5.2));
   if (launches(64, 64)) consider(kProductTiles64, cost(2.4 + std::max(1.0, quarter) * (nk * 0.21 + 0.9), 5.1));
   if (most_tiles(rows, grouped, experts, 16) > kSlimTiles || !launch_fits(((int64_t)N + 15) / 16, kThreads)) return best;
   if (by_k) {
@@ -665,6 +675,10 @@ hipError_t launch_product_kind(ProductKind kind, const ProductArgs& a, bool by_k
       return by_k ? launch_tiles<true, 64, 64>(a, s) : launch_tiles<false, 64, 64>(a, s);
     case kProductTiles128:
       return by_k ? launch_tiles<true, 128, 128>(a, s) : launch_tiles<false, 128, 128>(a, s);
+    case kProductTiles128x64:
+      return by_k ? launch_tiles<true, 128, 64>(a, s) : launch_tiles<false, 128, 64>(a, s);
+    case kProductDeep128:  // by row the tiles of 128 have as many steps
+      return by_k ? launch_tiles<true, 128, 128, 3>(a, s) : launch_tiles<false, 128, 128>(a, s);
     case kProductTiles256:
       return by_k ? launch_tiles<true, 256, 256>(a, s) : launch_tiles<false, 256, 256>(a, s);
   }

@@ -148,7 +148,7 @@ class DwPlan(ctypes.Structure):
     _fields_ = [("tile", ctypes.c_int), ("split", ctypes.c_int)]
 
 
-KINDS = ["slim1", "slim2", "tiles64", "tiles128", "tiles256"]
+KINDS = ["slim1", "slim2", "tiles64", "tiles128", "tiles256", "tiles128x64", "deep128"]
 
 
 def ptr(t):

@@ -183,9 +183,9 @@ def test_the_product_chosen_can_be_launched(rows, grouped, E, K, N, by_k):
     kind, ends = f(rows, grouped, E, K, N, by_k), E if grouped else 0
     if kind < 2:
         assert -(-rows // 16) + ends <= 65535 and -(-N // (64 if by_k else 16 << kind)) * 256 < 2 ** 32
-    elif kind < 4:
-        side = 64 if kind == 2 else 128
-        assert (-(-rows // side) + ends) * -(-N // side) * 256 < 2 ** 32
+    elif kind != 4:
+        w, x = {2: (64, 64), 3: (128, 128), 5: (128, 64), 6: (128, 128)}[kind]
+        assert (-(-rows // x) + ends) * -(-N // w) * 256 < 2 ** 32
 
 
 @pytest.mark.parametrize("rows,E,K,N", [(1, 1024, 2 ** 13, 2 ** 13), (64, 1, 2 ** 18, 2 ** 18), (2 ** 31 - 1, 1, 2 ** 18, 2 ** 18), (1, 1, 2 ** 18, 2 ** 17)])

@@ -57,7 +57,7 @@ def instructions(body):
     return ins, states, mine
 
 
-@pytest.mark.parametrize("kind,count", [("product_tile_kernel", 2), ("dw_tile_kernel", 2), ("product_small_kernel", 4), ("dw_small_kernel", 4),
+@pytest.mark.parametrize("kind,count", [("product_tile_kernel", 2), ("dw_tile_kernel", 2), ("product_small_kernel", 7), ("dw_small_kernel", 4),
                                         ("product_thin_kernel", 1)])
 def test_assembly_statements_keep_their_distances(kernels, kind, count):
     """Matrix instructions and LDS DMAs that are assembly statements: no vector instruction writes an operand within two
