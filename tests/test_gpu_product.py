@@ -211,6 +211,28 @@ def test_each_dw_kernel(counts, K, N, tile, split, gather):
     check_dw(host(dw), d)
 
 
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("tile,split", [(64, 1), (128, 1), (128, 2), (256, 1)])
+@pytest.mark.parametrize("counts,K,N", EACH, ids=lambda v: str(v)[:24])
+def test_each_dw_kernel_in_16_bits(counts, K, N, tile, split, gather):
+    """Nothing is written past dw, and a row that is not there shows in its expert's values alone."""
+    log(f"dw in bf16, tiles of {tile}, {split} parts {str(counts)[:60]} K={K} N={N} gather={gather}")
+    d = case(counts, K, N, gather, K * 11 + N)
+    if gather and d["end"] > 8:
+        d["index"][d["end"] // 2] = d["n"]
+        d["index_dev"] = torch.from_numpy(d["index"]).cuda()
+    f = B.load()._ZN3moe22launch_product_dw_planERKNS_6DwPlanERKNS_13ProductDwArgsEP12ihipStream_t
+    f.argtypes, f.restype = [ctypes.POINTER(DwPlan), ctypes.POINTER(ProductDwArgs), ctypes.c_void_p], ctypes.c_int
+    room, parts = filled((d["E"] * N * K + 1024,)), torch.full((split, d["E"], N, K), np.nan, device="cuda")
+    args = ProductDwArgs(ptr(d["dy_dev"]), ptr(d["x_dev"]), ptr(d["index_dev"]), ptr(d["off_dev"]), ptr(room), ptr(parts), d["n"],
+                         d["rows"], d["E"], K, N, 1, 0)
+    torch.cuda.synchronize()
+    assert f(ctypes.byref(DwPlan(tile, split)), ctypes.byref(args), torch.cuda.current_stream().cuda_stream) == 0
+    got = host(room)
+    assert (got[-1024:] == SENTINEL).all()
+    check_dw(got[:-1024].reshape(d["w"].shape), d, rounding=2.0 ** -8)
+
+
 @pytest.mark.parametrize("tile,split", [(64, 1), (64, 4), (128, 2), (256, 1), (256, 3)])
 def test_a_row_that_is_not_there_shows_in_its_experts_dw(tile, split):
     d = case([300, 40, 0, 700], 136, 264, True, 5)
