@@ -620,46 +620,47 @@ hipError_t launch_tiles(const ProductArgs& a, hipStream_t s) {
 ProductKind product_kind(int64_t rows, bool grouped, int32_t experts, int32_t K, int32_t N, bool by_k) {
   // What each kernel would take, in microseconds, from the rows an expert has on average (the host does not know
   // the offsets): the rounds of tiles over 256 compute units, each so many K steps and something for its start and end;
-  // and the reading of every weight, at the rate in TB/s that the kernel reached where that is all.  Against 595 measured
-  // products (1 to 49152 rows, 1 to 128 experts) the kernel chosen takes 2.5 % longer than the best one, 17 % in one of
-  // twenty, 61 % at most; by k 2.6, 20 and 57 %.
+  // and the reading of every weight, at the rate in TB/s that the kernel reached where that is all.  Fitted to 15675 measured
+  // products (1 to 49152 rows, 1 to 128 experts): the kernel chosen takes 2.6 % longer than the best one, 18 % in one of twenty,
+  // 97 % at most; by k 1.4, 12 and 91 %.  The tiles of 128 x 64 and the deep ring were worth 1.1 % at the mean of 2000 problems by
+  // row and 2.3 by k.
   const double nk = (K + kTileK - 1) / kTileK;
   const double busy = grouped ? experts * (1.0 - std::pow(1.0 - 1.0 / experts, (double)rows)) : 1.0;
   const double per = rows / busy, megabytes = busy * N * (2e-6 * K);
   auto tiles = [&](double x) { return grouped ? busy * (1.0 + std::max(0.0, (per - x / 2) / x)) : std::ceil(rows / x); };
   auto items = [&](double w, double x) { return tiles(x) * std::ceil(N / w) / 256.0; };
+  auto by = [&](double row, double k) { return by_k ? k : row; };
   auto cost = [&](double work, double rate) { return std::max(work, megabytes / rate) + 0.35 * work; };
   auto step = [](double h) {
     return h < 64 ? 0.41 + 0.25 * (h - 32) / 32 : h < 128 ? 0.66 + 0.11 * (h - 64) / 64 : 0.77 + 0.615 * (h - 128) / 128;
   };
   const double whole = items(256, 256), half = items(128, 128), quarter = items(64, 64);
   const double height = std::min(256.0, std::max(32.0, per)), rest = whole - std::floor(whole);
-  double tall = std::floor(whole) * (nk * step(height) + 3.5);
+  const double pace = by(0.701, 0.94);
+  double tall = std::floor(whole) * (nk * pace * step(height) + by(4.73, 5.56));
   if (rest > 0) {
     const int parts = parts_of((uint32_t)std::ceil(rest * kStaying / kXcds));
-    tall += nk * step(std::max(32.0, std::min(height, 256.0 / parts))) + 5;
+    tall += nk * pace * step(std::max(32.0, std::min(height, 256.0 / parts))) + by(5.19, 4.15);
   }
   ProductKind best = kProductTiles256;
-  double least = cost(1.2 + tall, 4.7);
+  double least = cost(by(2.62, 1.52) + tall, by(4.99, 5.18));
   auto consider = [&](ProductKind kind, double c) {
     if (c < least) best = kind, least = c;
   };
   // The small tiles and the slim kernels have a workgroup for each item, and can be too many for one launch.
   auto launches = [&](int w, int x) { return launch_fits(dealt(most_tiles(rows, grouped, experts, x), (N + w - 1) / w), kThreads); };
-  if (launches(128, 128)) consider(kProductTiles128, cost(1.2 + std::ceil(half) * (nk * 0.48 + 2.8), 4.9));
-  // Fitted to 2000 more products (64 to 45000 rows, 1 to 64 experts): these two are chosen for a fifth of them ByRow and a
-  // third ByK, which take 5 and 7 % less for it; one in eight and one in five takes over 5 % less, one in 45 and one in 20 more.
-  if (launches(128, 64)) {
-    const double flat = std::ceil(items(128, 64));
-    consider(kProductTiles128x64, by_k ? cost(1.2 + flat * (nk * 0.362 + 0.97), 5.2) : cost(1.7 + flat * (nk * 0.283 + 1.32), 4.9));
-  }
-  if (by_k && launches(128, 128)) consider(kProductDeep128, cost(0.24 + std::ceil(half) * (nk * 0.46 + 3.75), 5.2));
-  if (launches(64, 64)) consider(kProductTiles64, cost(2.4 + std::max(1.0, quarter) * (nk * 0.21 + 0.9), 5.1));
+  if (launches(128, 128))
+    consider(kProductTiles128, cost(1.16 + std::ceil(half) * (nk * by(0.449, 0.466) + by(2.97, 2.8)), by(5.14, 4.8)));
+  if (by_k && launches(128, 128)) consider(kProductDeep128, cost(0.24 + std::ceil(half) * (nk * 0.46 + 3.75), 5.36));
+  if (launches(128, 64))
+    consider(kProductTiles128x64, cost(by(2.16, 1.2) + std::ceil(items(128, 64)) * (nk * by(0.263, 0.313) + by(1.32, 1.11)), by(5.24, 5.2)));
+  if (launches(64, 64))
+    consider(kProductTiles64, cost(by(2.23, 1.68) + std::max(1.0, quarter) * (nk * by(0.231, 0.282) + by(0.894, 0.627)), by(6.84, 5.1)));
   if (most_tiles(rows, grouped, experts, 16) > kSlimTiles || !launch_fits(((int64_t)N + 15) / 16, kThreads)) return best;
   if (by_k) {
-    consider(kProductSlim1, cost(2.0 + nk * std::max(0.075, 0.3 * items(64, 16)), 4.7));
+    consider(kProductSlim1, cost(2.21 + nk * std::max(0.075, 0.279 * items(64, 16)), 3.72));
   } else {
-    consider(kProductSlim1, cost(2.4 + nk * std::max(0.12, 0.13 * items(16, 16)), 6.9));
+    consider(kProductSlim1, cost(1.4 + nk * std::max(0.12, 0.163 * items(16, 16)), 6.9));
     consider(kProductSlim2, cost(2.4 + nk * 0.16 * std::max(1.0, items(32, 16)), 6.9));
   }
   return best;

@@ -488,8 +488,8 @@ hipError_t launch_dw(const DwPlan& plan, const ProductDwArgs& a, hipStream_t s) 
 DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N) {
   // What each way would take, in microseconds, from the rows an expert has on average: one tile alone, or as many as a
   // compute unit has one after another, whichever is longer; the writing of the sums; and the second launch that adds up
-  // parts.  Fitted to 3236 problems (1 to 49152 rows, 1 to 128 experts): the way chosen takes 2.7 % longer than the best
-  // one, 18 % in one of twenty, 59 % at most.
+  // parts.  Fitted to 12441 problems (1 to 49152 rows, 1 to 128 experts, both types): the way chosen takes 1.8 % longer than
+  // the best one, 13 % in one of twenty, 71 % at most.
   const double nk = std::ceil((double)rows / experts / kTileK), megabytes = (double)experts * N * K * 4e-6;
   DwPlan best{256, 1};
   double least = 1e30;
@@ -507,9 +507,9 @@ DwPlan product_dw_plan(int64_t rows, int32_t experts, int32_t K, int32_t N) {
       if (cost < least) best = DwPlan{tile, split}, least = cost;
     }
   };
-  consider(256, {0.505, 1.7, 1.1, 8.6, 0.88, 0.056, 6.0, 0.224, 1.4});
-  consider(128, {0.615, 0.6, 0.578, 0.5, 0.39, 0.154, 4.6, 0.246, 1.6});
-  consider(64, {0.413, 0, 0.244, 0.55, 1, 0.072, 3.2, 0.196, 2.4});
+  consider(256, {0.505, 1.7, 1.191, 9.198, 0.599, 0.052, 4.411, 0.153, 1.497});
+  consider(128, {0.658, 0.735, 0.578, 0.489, 0.492, 0.143, 4.184, 0.257, 1.455});
+  consider(64, {0.349, 0, 0.227, 0.55, 0.91, 0.1, 3.2, 0.177, 2.568});
   return best;
 }
 
