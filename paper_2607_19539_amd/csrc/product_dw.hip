@@ -8,7 +8,7 @@
 //
 // The sums' writing bounds it as much as the products do: 8 experts of some 1024 rows by 4096 x 14336 (1.88 GB of fp32) take
 // 940 us, 720 without the stores, and 64 of some 768 by 2816 x 2048 (1.48 GB) 670 and 496; one matrix of 8192 x 8192 x
-// 8192 755 us (1.46 PFLOP/s; the library's product into bf16 1017, here 712).  Tried without gain: stores past the
+// 8192 755 us (1.46 PFLOP/s; into bf16 733, the library's product 939).  Tried without gain: stores past the
 // caches (2 to 15 % slower), stores whose lanes lie next to each other (the same, though one compute unit alone then
 // stores three times as fast), workgroups out of step with one another by a part of a tile (0 to 5 % slower: their
 // reads no longer meet in L2), waits that let the stores pass (the same).
