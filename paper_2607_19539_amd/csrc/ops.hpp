@@ -178,6 +178,9 @@ hipError_t launch_squares(const TensorTable<kMost>& t, double* parts, int blocks
 hipError_t launch_squares_sum(const double* parts, int n, double* total, hipStream_t s);
 template <int kMost>
 hipError_t launch_clip(const TensorTable<kMost>& t, const double* total, float max_norm, float* norm, int blocks, hipStream_t s);
+// Waves that share a choice: 1 or 4.
+int combine_backward_parts(int64_t choices, int32_t H);
+hipError_t launch_combine_backward_parts(int parts, const CombineBackwardArgs& a, hipStream_t s);
 hipError_t launch_combine_backward(const CombineBackwardArgs& a, hipStream_t s);
 
 }  // namespace moe

@@ -74,6 +74,21 @@ def test_a_row_that_a_token_names_more_than_once():
     check(bf16(rng, 4, 520), bf16(rng, 9, 520), slot, rng.random((4, 4)).astype(np.float32))
 
 
+@pytest.mark.parametrize("T,k,H", [(1, 1, 4096), (128, 8, 4104), (129, 8, 4104), (60, 3, 8200), (5, 7, 16384), (64, 16, 4088)])
+def test_long_rows_of_few_and_of_many_choices(T, k, H):
+    """One wave a choice and four, with slots that are not there and rows that a token names more than once."""
+    log(f"combine backward, long rows {T} x {k} x {H}")
+    rng = np.random.default_rng(T * k + H)
+    slot = rng.permutation(T * k).astype(np.int32).reshape(T, k)
+    if k > 2:
+        slot[::3, 1], slot[1::3, 2], slot[T - 1, k - 1] = -1, slot[1::3, 0], T * k
+    gate = rng.random((T, k)).astype(np.float32)
+    dout, recv = bf16(rng, T, H), bf16(rng, T * k, H)
+    check(dout, recv, slot, gate)
+    check(dout, recv, slot, gate, want_drecv=False)
+    check(dout, recv, slot, gate, want_dgate=False, stream=torch.cuda.Stream())
+
+
 def test_gradients_by_differences():
     """Against moe_combine: out moves by gate times what recv moves, and by recv times what gate moves, off by two
     roundings of out to bf16, 2^-8 each."""
