@@ -73,7 +73,7 @@ struct Experts {
       hi = m;
       if (!have) lo = hi;
     }
-    end = b.tiles + scan_add((uint32_t)(hi - lo + kTile - 1) / kTile);
+    end = b.tiles + scan_add(((uint32_t)(hi - lo) + kTile - 1) / kTile);
   }
   template <class Args>
   __device__ __forceinline__ Before after(const Args& a, int e0) const {

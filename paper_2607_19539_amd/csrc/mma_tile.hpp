@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "plan_types.hpp"
+#include "row_parts.hpp"
 
 namespace moe {
 
@@ -162,7 +163,7 @@ struct IndexAhead {
   __device__ __forceinline__ void load(const int32_t* index, int n, int step) {
     const int lane = (int)(threadIdx.x & 63);
 #pragma unroll
-    for (int u = 0; u < kIndexSteps; ++u) row[u] = index[min(min((step + u) * kTileK, max(n - kTileK, 0)) + lane, n - 1)];
+    for (int u = 0; u < kIndexSteps; ++u) row[u] = index[row_of_step(step + u, lane, n)];
   }
   __device__ __forceinline__ void arrived() {  // waited for here: later waits for one each would wait for the DMAs between them
 #pragma unroll
@@ -310,7 +311,7 @@ struct ChunkTail {  // int8
 // the operand.  Elements outside [lo, hi) are zeroed in both operands, since either may hold infinities there.
 struct ElementTail {
   static constexpr bool partial = true;
-  static __device__ __forceinline__ int steps(int K) { return (K + kTileK - 1) / kTileK; }
+  static __device__ __forceinline__ int steps(int K) { return steps_of(K); }
   uint32_t bytes_w, bytes_x;
   int lo, hi;
   // step_w, step_x: bytes from one k to the next of each operand.

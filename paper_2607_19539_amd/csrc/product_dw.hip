@@ -25,6 +25,7 @@
 #include "launch.hpp"
 #include "mma_tile.hpp"
 #include "ops.hpp"
+#include "row_parts.hpp"
 #include "vec_device.hpp"
 
 namespace moe {
@@ -73,10 +74,8 @@ __device__ __forceinline__ DwItem dw_item(const ProductDwArgs& a, ExpertRows& ex
   const uint32_t band = q / (kBandTiles * tk), in = q % (kBandTiles * tk), nb = min((uint32_t)kBandTiles, tn - band * kBandTiles);
   int lo, hi;
   experts.of(a, e, lo, hi);
-  // Parts of whole K steps.
-  const int steps = (hi - lo + kTileK - 1) / kTileK, each = (steps + split - 1) / split * kTileK;
-  const int row0 = min(lo + part * each, hi);
-  return DwItem{e, part, (int)(band * kBandTiles + in % nb) * kTile, (int)(in / nb) * kTile, row0, min(each, hi - row0)};
+  const RowPart rows = row_part(lo, hi, split, part);
+  return DwItem{e, part, (int)(band * kBandTiles + in % nb) * kTile, (int)(in / nb) * kTile, rows.row0, rows.rows};
 }
 
 __device__ __forceinline__ DwItem uniform(const DwItem& it) {
