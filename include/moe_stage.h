@@ -620,6 +620,7 @@ int moe_gate_backward(const void* gu, const void* dact, const int32_t* expert_of
  * A slot outside [0, recv_rows) has no row: its dgate is 0.  Rows of drecv that no slot names are not
  * written.  A row that one token names more than once gets the sum of its gates.  Different tokens have
  * different rows, as in moe_group's slot; a row that two of them named would get the gradient of either.
+ * drecv may be recv itself, and overlaps nothing else.
  * hidden: a multiple of 8, at most 65536; k: at most 64.
  */
 int moe_combine_backward(const void* dout, const void* recv, int64_t recv_rows, int32_t hidden, const int32_t* slot,

@@ -718,8 +718,8 @@ def moe_gate_backward(gu, dact, dgu, act=None, expert_offsets=None, stream=None)
 
 
 def moe_combine_backward(dout, recv, slot, gate, drecv=None, dgate=None, stream=None) -> int:
-    """Gradients of moe_combine: drecv [rows, H] bf16 and dgate [T, k] fp32 from dout [T, H] and the call's recv, slot
-    and gate."""
+    """Gradients of moe_combine: drecv [rows, H] bf16 (recv itself will do) and dgate [T, k] fp32 from dout [T, H] and the
+    call's recv, slot and gate."""
     T, H = _rows_of("dout", dout)
     rows, _ = _rows_of("recv", recv)
     _, k = _rows_of("slot", slot)

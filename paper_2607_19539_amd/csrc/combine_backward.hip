@@ -36,14 +36,15 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineBackw
     if (a.dgate && lane == 0 && part == 0) a.dgate[choice] = 0.0f;
     return;
   }
-  // A row that a token names more than once takes all of its gates, through the first of them.
+  // A row that a token names more than once takes all of its gates, through the first of them, which does the others' work:
+  // their dgate is the same sum, and drecv may be recv, whose row nobody may read when the first has begun to write it.
   float gate = a.gate[choice];
-  bool write = a.drecv != nullptr;
+  const bool write = a.drecv != nullptr;
+  uint64_t same = 1ull << j;
   if (a.k > 1 && write) {
-    const uint64_t same = __ballot(lane < a.k && a.slot[t * a.k + min(lane, a.k - 1)] == slot);
-    uint64_t more = same & ~(1ull << j);
-    write = (same & ((1ull << j) - 1)) == 0;
-    for (; more && write; more &= more - 1) gate += a.gate[t * a.k + __builtin_ctzll(more)];
+    same = __ballot(lane < a.k && a.slot[t * a.k + min(lane, a.k - 1)] == slot);
+    if (same & ((1ull << j) - 1)) return;
+    for (uint64_t more = same & ~(1ull << j); more; more &= more - 1) gate += a.gate[t * a.k + __builtin_ctzll(more)];
   }
   const uint16_t* dout = a.dout + t * H;
   const uint16_t* recv = a.recv + (int64_t)slot * H;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineBackw
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) sum += sums[w];
     }
-    if (lane == 0 && part == 0) a.dgate[choice] = sum;
+    if (part == 0 && (same >> lane & 1)) a.dgate[t * a.k + lane] = sum;
   }
 }
 
