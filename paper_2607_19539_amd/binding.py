@@ -362,6 +362,11 @@ def _current_stream():
     return lambda: torch.cuda.current_stream().cuda_stream
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         return _current_stream()()
@@ -518,11 +523,14 @@ def _rows_of(name, t):
     return t.shape
 
 
-def _workspace(given, need, stream):
-    """The caller's workspace, or one from torch's allocator, taken on the stream that will use it."""
+def _workspace(given, need, stream, here=False):
+    """The caller's workspace, or one from torch's allocator, taken on the stream that will use it.  ``here``: the
+    caller's has to be on the current device."""
     if given is not None:
         if not given.is_cuda or not given.is_contiguous():
             raise ValueError("workspace must be a contiguous device tensor")
+        if here and given.device.index != _current_device():
+            raise ValueError("workspace must be a contiguous device tensor on the current device")
         return given, given.numel() * given.element_size()
     if need <= 0:
         return None, 0
@@ -639,6 +647,14 @@ def moe_q8_gated(xq, x_scale, w1, w1_scale, w3, w3_scale, out, row_index=None, e
     return _check(load().moe_q8_gated(*lead, *mats, *more, *tail, _stream_ptr(stream)))
 
 
+def _stream_here(stream) -> Optional[int]:
+    """_stream_ptr of a stream of the current device: a kernel runs on its stream's, where the tensors (_HERE) are not."""
+    device = getattr(stream, "device_index", None)   # of torch's streams; a handle does not tell
+    if device is not None and device != _current_device():
+        raise ValueError("stream must be one of the current device")
+    return _stream_ptr(stream)
+
+
 def _matrices(name, t):
     if len(t.shape) != 3:
         raise ValueError(f"{name} must have three dimensions, got {list(t.shape)}")
@@ -662,7 +678,7 @@ def moe_product(x, w, out, row_index=None, expert_offsets=None, stream=None) -> 
     off = _offsets(expert_offsets, E)
     return _check(load().moe_product(
         _want("x", x, (n, K), _BITS16_HERE), n, _opt("row_index", row_index, (rows,), _INT32_HERE), off, E,
-        _want("w", w, (E, N, K), _BITS16_HERE), rows, K, N, _want("out", out, (rows, N), _BITS16_HERE), _stream_ptr(stream)))
+        _want("w", w, (E, N, K), _BITS16_HERE), rows, K, N, _want("out", out, (rows, N), _BITS16_HERE), _stream_here(stream)))
 
 
 def moe_product_dx(dy, w, dx, expert_offsets=None, stream=None) -> int:
@@ -672,7 +688,7 @@ def moe_product_dx(dy, w, dx, expert_offsets=None, stream=None) -> int:
     off = _offsets(expert_offsets, E)
     return _check(load().moe_product_dx(
         _want("dy", dy, (rows, N), _BITS16_HERE), off, E, _want("w", w, (E, N, K), _BITS16_HERE), rows, K, N,
-        _want("dx", dx, (rows, K), _BITS16_HERE), _stream_ptr(stream)))
+        _want("dx", dx, (rows, K), _BITS16_HERE), _stream_here(stream)))
 
 
 def moe_product_dw(dy, x, dw, row_index=None, expert_offsets=None, accumulate=False, workspace=None, stream=None) -> int:
@@ -688,8 +704,9 @@ def moe_product_dw(dy, x, dw, row_index=None, expert_offsets=None, accumulate=Fa
     args = (_want("dy", dy, (rows, N), _BITS16_HERE), _want("x", x, (n, K), _BITS16_HERE), n,
             _opt("row_index", row_index, (rows,), _INT32_HERE), off, E, rows, K, N,
             _want("dw", dw, (E, N, K), _LOGITS_HERE), kind, int(bool(accumulate)))
-    ws, size = _workspace(workspace, lib.moe_product_dw_workspace(rows, E, K, N), stream)
-    return _check(lib.moe_product_dw(*args, ws if ws is None else ws.data_ptr(), size, _stream_ptr(stream)))
+    on = _stream_here(stream)
+    ws, size = _workspace(workspace, lib.moe_product_dw_workspace(rows, E, K, N), stream, here=True)
+    return _check(lib.moe_product_dw(*args, ws if ws is None else ws.data_ptr(), size, on))
 
 
 def _gate_rows(gu, expert_offsets):
@@ -705,7 +722,7 @@ def moe_gate(gu, act, expert_offsets=None, stream=None) -> int:
     of expert_offsets are left alone."""
     rows, F, off, E = _gate_rows(gu, expert_offsets)
     return _check(load().moe_gate(_want("gu", gu, (rows, 2 * F), _BITS16_HERE), off, E, rows, F,
-                                  _want("act", act, (rows, F), _BITS16_HERE), _stream_ptr(stream)))
+                                  _want("act", act, (rows, F), _BITS16_HERE), _stream_here(stream)))
 
 
 def moe_gate_backward(gu, dact, dgu, act=None, expert_offsets=None, stream=None) -> int:
@@ -714,7 +731,7 @@ def moe_gate_backward(gu, dact, dgu, act=None, expert_offsets=None, stream=None)
     rows, F, off, E = _gate_rows(gu, expert_offsets)
     return _check(load().moe_gate_backward(
         _want("gu", gu, (rows, 2 * F), _BITS16_HERE), _want("dact", dact, (rows, F), _BITS16_HERE), off, E, rows, F,
-        _want("dgu", dgu, (rows, 2 * F), _BITS16_HERE), _opt("act", act, (rows, F), _BITS16_HERE), _stream_ptr(stream)))
+        _want("dgu", dgu, (rows, 2 * F), _BITS16_HERE), _opt("act", act, (rows, F), _BITS16_HERE), _stream_here(stream)))
 
 
 def moe_combine_backward(dout, recv, slot, gate, drecv=None, dgate=None, stream=None) -> int:
@@ -726,7 +743,7 @@ def moe_combine_backward(dout, recv, slot, gate, drecv=None, dgate=None, stream=
     return _check(load().moe_combine_backward(
         _want("dout", dout, (T, H), _BITS16_HERE), _want("recv", recv, (rows, H), _BITS16_HERE), rows, H,
         _want("slot", slot, (T, k), _INT32_HERE), _want("gate", gate, (T, k), _F32_HERE), T, k,
-        _opt("drecv", drecv, (rows, H), _BITS16_HERE), _opt("dgate", dgate, (T, k), _F32_HERE), _stream_ptr(stream)))
+        _opt("drecv", drecv, (rows, H), _BITS16_HERE), _opt("dgate", dgate, (T, k), _F32_HERE), _stream_here(stream)))
 
 
 def _tensor_list(tensors, out=None):
@@ -742,8 +759,9 @@ def moe_squares(tensors, total, workspace=None, stream=None) -> int:
     entries, n = _tensor_list(tensors)
     lib = load()
     ptr = _want("total", total, (1,), _F64_HERE)
-    ws, size = _workspace(workspace, lib.moe_squares_workspace(entries, n), stream)
-    return _check(lib.moe_squares(entries, n, ptr, ws if ws is None else ws.data_ptr(), size, _stream_ptr(stream)))
+    on = _stream_here(stream)
+    ws, size = _workspace(workspace, lib.moe_squares_workspace(entries, n), stream, here=True)
+    return _check(lib.moe_squares(entries, n, ptr, ws if ws is None else ws.data_ptr(), size, on))
 
 
 def moe_clip(tensors, total, max_norm, out=None, norm=None, stream=None) -> int:
@@ -751,7 +769,7 @@ def moe_clip(tensors, total, max_norm, out=None, norm=None, stream=None) -> int:
     fp64 is their sum of squares; the norm before it in ``norm`` [1] fp32."""
     entries, n = _tensor_list(tensors, out)
     return _check(load().moe_clip(entries, n, _want("total", total, (1,), _F64_HERE), max_norm,
-                                  _opt("norm", norm, (1,), _F32_HERE), _stream_ptr(stream)))
+                                  _opt("norm", norm, (1,), _F32_HERE), _stream_here(stream)))
 
 
 def moe_stage_query(h, check: bool = True) -> dict:
