@@ -465,13 +465,13 @@ __device__ __forceinline__ void tile_start(uint8_t* __restrict__ lds, W& w, DmaR
 }
 
 // The K loop after tile_start: late() two K steps (or one) before the end, last() before the last step, when every
-// DMA has arrived.
-template <class Op, class LayoutW = ByRow, class LayoutX = ByRow, int kNJ, class W, class Tail, class Late, class Last>
-__device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRows<kNJ>& x, int K, const Tail& tail,
-                                         typename Op::Acc (&acc)[8][kNJ], Late&& late, Last&& last) {
+// DMA has arrived.  Operands ByRow, whose K ends with a step or a chunk.
+template <class Op, int kNJ, class Tail, class Late, class Last>
+__device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, DmaRows<kDmaPerThread>& w, DmaRows<kNJ>& x, int K,
+                                         const Tail& tail, typename Op::Acc (&acc)[8][kNJ], Late&& late, Last&& last) {
   typedef typename Op::Frag Frag;
   static_assert(kNJ == 4 || kNJ == 6 || kNJ == 8, "token fragments per wave");
-  static_assert(!LayoutX::transposed || kNJ != 6, "a wave's tokens start on half a panel or on a panel");
+  static_assert(!std::is_same_v<Tail, ElementTail>, "TileStream's");
   constexpr int kHJ = kNJ / 2;
   const int tid = item_thread(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -489,8 +489,8 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRow
   // Ring slots by block: o0, o1 hold K step ks's weights and tokens, o2 and o3 step ks+1's, o4 takes
   // step ks+2's weights and o0, once read, its tokens.  They rotate by two per step.
   uint32_t o0 = 0, o1 = kBlockBytes, o2 = 2 * kBlockBytes, o3 = 3 * kBlockBytes, o4 = 4 * kBlockBytes;
-  const Fragments<LayoutW, Frag> a_lane((uint32_t)(wn * 128), lane);
-  const Fragments<LayoutX, Frag> b_lane((uint32_t)(wm * 16 * kNJ), lane);
+  const Fragments<ByRow, Frag> a_lane((uint32_t)(wn * 128), lane);
+  const Fragments<ByRow, Frag> b_lane((uint32_t)(wm * 16 * kNJ), lane);
   Frag fa[8], fb[kNJ];
   auto read_a = [&](uint32_t slot, int kk, int i) { fa[i] = a_lane.read(lds, slot, kk, i * 16); };
   auto read_b = [&](uint32_t slot, int kk, int j) { fb[j] = b_lane.read(lds, slot, kk, j * 16); };
@@ -554,24 +554,11 @@ __device__ __forceinline__ void tile_run(uint8_t* __restrict__ lds, W& w, DmaRow
     using steady = std::integral_constant<bool, kd == 0>;
     using first = std::integral_constant<int, 0>;
     using second = std::integral_constant<int, 1>;
-    // In the last step, the elements that it does not hold: of what half 0 multiplies, then of half 1's.
-    auto mask0 = [&](int kk) {
-      if constexpr (kd == 2) {
-        mask_chunks(tail, kk, lk, fa);
-        mask_elements(tail, kk, lk, fa, 0, 8);
-        mask_elements(tail, kk, lk, fb, 0, kHJ);
-      }
-    };
-    auto mask1 = [&](int kk) {
-      if constexpr (kd == 2) mask_elements(tail, kk, lk, fb, kHJ, kHJ);
-    };
-    mask0(0);
+    if constexpr (kd == 2) mask_chunks(tail, 0, lk, fa);
     half0(first{}, steady{});
-    mask1(0);
     half1(o0, o1, second{}, std::true_type{}, steady{});
-    mask0(1);
+    if constexpr (kd == 2) mask_chunks(tail, 1, lk, fa);
     half0(second{}, std::false_type{});
-    mask1(1);
     if constexpr (kd < 2) wait_vm_and_barrier<kd == 0 ? kDmaPerThread : 0>();  // step ks+1 visible, step ks's slots free
     half1(o2, o3, first{}, std::integral_constant<bool, (kd < 2)>{}, steady{});
     if constexpr (kd == 0) advance_to(w, x, ks + 3, nk, tail);
