@@ -649,6 +649,8 @@ def moe_q8_gated(xq, x_scale, w1, w1_scale, w3, w3_scale, out, row_index=None, e
 
 def _stream_here(stream) -> Optional[int]:
     """_stream_ptr of a stream of the current device: a kernel runs on its stream's, where the tensors (_HERE) are not."""
+    if stream is None:
+        return _current_stream()()
     device = getattr(stream, "device_index", None)   # of torch's streams; a handle does not tell
     if device is not None and device != _current_device():
         raise ValueError("stream must be one of the current device")
