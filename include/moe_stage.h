@@ -554,7 +554,7 @@ int moe_q8_gated(const void* xq, const float* x_scale, int64_t x_rows, const int
  * What trains a layer of experts: the 16-bit products and their gradients, the
  * gated activation, the combine's gradient, and the norm of all gradients.  They
  * behave as the operators above do.  (A row of moe_gate has ffn / 8 threads, a
- * choice of moe_combine_backward 64.)
+ * choice of moe_combine_backward 64, or 256 where there are few of long rows.)
  * ------------------------------------------------------------------------- */
 
 /*
@@ -600,7 +600,7 @@ int moe_product_dw(const void* dy, const void* x, int64_t x_rows, const int32_t*
  * The gated activation of rows that hold g and u side by side, as a product with the gate's and the up
  * weights one after another leaves them: gu [rows, 2 ffn] bf16, g the first ffn of a row;
  *   act = bf16( silu(g) * u )                     act [rows, ffn] bf16
- * and its gradient, with s = 1 / (1 + e^-g):
+ * and its gradient, with s = 1 / (1 + e^-g), 0 for g below -88.7, where e^-g passes fp32:
  *   dgu = bf16( dact * u * s * (1 + g * (1 - s)) ), bf16( dact * silu(g) )       dgu [rows, 2 ffn] bf16
  * dgu may be gu itself.  moe_gate_backward's act (optional) is moe_gate's again, for a program that does
  * not keep it.  expert_offsets (optional, device, [experts + 1]): rows at or past expert_offsets[experts]

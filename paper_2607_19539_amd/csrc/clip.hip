@@ -5,8 +5,10 @@
 // Squares are taken and added in 64 bits: no gradient is too large or too small for its square, and the order of the
 // sum does not show in the 32-bit norm.  Memory bounds both passes: 1.1e9 elements of both types (3.3 GB) are read in 570 us
 // (5.8 TB/s), and read and written in 1290 (5.1 TB/s).  Chunks of a 2048th of the whole, as many as there are workgroups,
-// took 940 and 1670: the last ones of a launch leave compute units idle, and a thread had one piece in flight, not four.  The tensors' addresses travel in the kernel's
-// arguments, so nothing is copied before a launch and a captured launch keeps them.
+// took 940 and 1670: the last ones of a launch leave compute units idle, and a thread had one piece in flight.  Now it has
+// four where a chunk has as many left: of fp32 always, of bf16 in chunks of 8192 elements or more (a list below 2^28 elements
+// has chunks of 4096, two pieces one after another).  The tensors' addresses travel in the kernel's arguments, so nothing is
+// copied before a launch and a captured launch keeps them.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
