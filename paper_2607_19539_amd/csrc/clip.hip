@@ -127,9 +127,12 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable<kMost> t, co
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
   // A norm that is not finite, or not as the caller sees it in 32 bits, leaves the gradients as they are.
   const double ratio = root > (double)max_norm && (float)root < __builtin_huge_valf() ? (double)max_norm / root : 1.0;
-  // In 32 bits a ratio below 2^-126 would lose bits of its own.  It goes in two steps, the first a power of two that is
-  // exact for every value that the ratio does not take below 2^-152, which is 0 in either type.
-  const float first = ratio < 0x1p-126 ? 0x1p-100f : 1.0f, scale = (float)(ratio / (double)first);
+  // In 32 bits a ratio below 2^-126 would lose bits of its own (it may be as small as 2^-277).  It goes in two steps then, a
+  // power of two that leaves 2^-100 or so of it: exact for every value that the ratio does not take below 2^-150, half of
+  // the smallest one, as those are 2^-74 or more after it.
+  const int shift = ratio > 0 && ratio < 0x1p-126 ? ilogb(ratio) + 100 : 0;
+  const float scale = (float)ldexp(ratio, -shift);
+  auto scaled = [&](float f) { return ldexpf(f, shift) * scale; };
   const int lane = threadIdx.x & 63;
   const uint32_t first0 = first_of(t, lane), first1 = first_of(t, lane + 64);
   for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
@@ -142,13 +145,13 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable<kMost> t, co
     if (bf16) {
       const uint16_t* v = (const uint16_t*)in + p.from;
       uint16_t* o = (uint16_t*)to + p.from;
-      auto one = [&](int64_t i) { o[i] = (uint16_t)bf16x2_of(f32_of(v[i]) * first * scale, 0.0f); };
+      auto one = [&](int64_t i) { o[i] = (uint16_t)bf16x2_of(scaled(f32_of(v[i])), 0.0f); };
       if (alike)
         pieces(v, p.n, [&](int64_t i, const u32x4& piece) {
           float f[8];
           unpack8(piece, f);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] = f[q] * first * scale;
+          for (int q = 0; q < 8; ++q) f[q] = scaled(f[q]);
           *(u32x4*)(o + i) = pack8(f);
         }, one);
       else
@@ -156,9 +159,14 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable<kMost> t, co
     } else {
       const float* v = (const float*)in + p.from;
       float* o = (float*)to + p.from;
-      auto one = [&](int64_t i) { o[i] = v[i] * first * scale; };
+      auto one = [&](int64_t i) { o[i] = scaled(v[i]); };
       if (alike)
-        pieces(v, p.n, [&](int64_t i, const u32x4& piece) { *(f32x4*)(o + i) = __builtin_bit_cast(f32x4, piece) * first * scale; }, one);
+        pieces(v, p.n, [&](int64_t i, const u32x4& piece) {
+          f32x4 f = __builtin_bit_cast(f32x4, piece);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) f[q] = scaled(f[q]);
+          *(f32x4*)(o + i) = f;
+        }, one);
       else
         for (int64_t i = threadIdx.x; i < p.n; i += kThreads) one(i);
     }
